@@ -185,6 +185,38 @@ int fc_view_create(const int32_t* cu_seqlens, int32_t n_docs, const fc_shard* sh
                    int64_t n_shards, int32_t cp, int32_t rank, int32_t hq, int32_t hkv,
                    int32_t d, const fc_tile_cfg* tiles, fc_view* out);
 
+/* A function of the scores between the product and the softmax, for every query
+ * head h, in this order:
+ *   cap     0: none; else s = cap * tanh(scale q.k / cap), FC_CAP_MIN <= cap <=
+ *           FC_CAP_MAX;
+ *   slopes  host, hq values, NULL: none; s -= slopes[h] * distance, the distance
+ *           being the query's position less the key's in their document; 0 <=
+ *           slopes[h] <= FC_SLOPE_MAX. A document of a view with slopes has at most
+ *           2^24 tokens (FC_ERR_UNSUPPORTED).
+ * Slopes and cap are constants: the backward has no gradient for them. */
+#define FC_CAP_MIN 0.015625f
+#define FC_CAP_MAX 1024.0f
+#define FC_SLOPE_MAX 1024.0f
+typedef struct {
+  float cap;
+  const float* slopes;
+} fc_score;
+
+/* fc_view_create for attention with capped and/or biased scores (NULL, or no cap
+ * and no slopes: fc_view_create). The view carries the function: its tables hold
+ * the slopes and the positions a bias counts, and every forward and backward call
+ * below applies it; lse is the log-sum-exp of the scores it gives, and dq, dk are
+ * the gradients through it. Inputs are finite, as for every view. Accuracy is that
+ * of the uncapped calls: a capped score is within cap * 2^-21 of its value, and
+ * 1 - tanh^2 is rounded to fp16 before dK's dS is rounded to bf16. */
+int fc_view_create_scored(const int32_t* cu_seqlens, int32_t n_docs, const fc_shard* shards,
+                          int64_t n_shards, int32_t cp, int32_t rank, int32_t hq, int32_t hkv,
+                          int32_t d, const fc_tile_cfg* tiles, const fc_score* score, fc_view* out);
+
+/* A view's cap (0: none), whether it has slopes, and these (host, hq values, 0
+ * without; any pointer may be NULL). */
+int fc_view_get_score(fc_view view, float* cap, int32_t* biased, float* slopes);
+
 int fc_view_get_info(fc_view view, fc_view_info* out);
 
 /* Copy the view's tables to host arrays (any pointer may be NULL):
@@ -282,6 +314,71 @@ int fc_workspace_size(fc_view view, int32_t mode, size_t* fwd_bytes, size_t* bwd
  * local pass as in Sec. 3.2); at least one part must be given. */
 int fc_kv_gather(fc_view view, const void* k_packed, const void* v_packed, int64_t t_packed,
                  void* k_loc, void* v_loc, void* k_recv, void* v_recv, void* stream);
+
+/* ---------------------------------------------------------------- rotary rows
+ * Rotary positions: pair i of a head's first `dim` values, (x_i, x_{i+dim/2}) or,
+ * interleaved, (x_2i, x_2i+1), is turned by the token's position times inv_freq[i]
+ * and multiplied by `amplitude`; the other values are left as they are. Positions
+ * count within the token's document, or (packed_pos) in the packed sequence. */
+typedef struct {
+  int32_t dim;            /* even, 2 .. d */
+  int32_t interleaved;    /* 0: halves apart, 1: neighbours */
+  int32_t packed_pos;
+  float amplitude;        /* finite; 1 but for some long-context scalings */
+  const double* inv_freq; /* host, dim/2: radians per position, |w| <= FC_ROPE_FREQ_MAX */
+} fc_rope;
+#define FC_ROPE_FREQ_MAX 8.0
+
+/* How frequencies w_i = base^(-2i/dim) are scaled for contexts `factor` times as
+ * long as the `context` a model was trained on:
+ *   FC_ROPE_NONE    not at all;
+ *   FC_ROPE_LINEAR  w_i / factor;
+ *   FC_ROPE_BASE    base * factor^(dim/(dim-2)) for the base (dim > 2);
+ *   FC_ROPE_BANDS   w_i / factor where a pair makes fewer than `low` turns in the
+ *                   trained context, w_i where it makes more than `high`, and a
+ *                   mean of both, linear in the turns, between;
+ *   FC_ROPE_YARN    the same with a mean linear in i, from the pair that makes
+ *                   `high` turns (rounded down) to the one that makes `low` (up),
+ *                   and amplitude 0.1 ln(factor) + 1. */
+enum { FC_ROPE_NONE = 0, FC_ROPE_LINEAR = 1, FC_ROPE_BASE = 2, FC_ROPE_BANDS = 3, FC_ROPE_YARN = 4 };
+
+/* Fills inv_freq[dim/2] (host) and *amplitude. base > 1; factor >= 1; low < high
+ * and context (tokens, > 0) are read by FC_ROPE_BANDS and FC_ROPE_YARN only. */
+int fc_rope_freqs(int32_t dim, double base, int32_t scaling, double factor, double low, double high,
+                  double context, double* inv_freq, float* amplitude);
+
+/* A tensor's rows on their way: token r's heads * d values from in + r * in_stride
+ * to out + r * out_stride (strides in elements, a multiple of 16 bytes; 0: rows
+ * without gaps, heads * d), so either may be a slice of a fused projection buffer.
+ * In place: the same address, stride and type. Otherwise no output may overlap an
+ * input or another output (FC_ERR_INVALID_ARG). */
+typedef struct {
+  const void* in;
+  int64_t in_stride;
+  void* out;
+  int64_t out_stride;
+} fc_rows;
+
+/* The rank's own rows, bf16, in one launch: q [T_q, Hq, d] and k [T_q, Hkv, d]
+ * rotated, v [T_q, Hkv, d] copied. Each of the three may be NULL (not all); rope
+ * NULL copies q and k too. */
+int fc_rope_fwd(fc_view view, const fc_rope* rope, const fc_rows* q, const fc_rows* k,
+                const fc_rows* v, void* stream);
+
+/* fc_kv_gather with the keys rotated on the way (rope NULL: fc_kv_gather). No
+ * output may overlap the packed tensors. */
+int fc_kv_gather_rope(fc_view view, const fc_rope* rope, const void* k_packed, const void* v_packed,
+                      int64_t t_packed, void* k_loc, void* v_loc, void* k_recv, void* v_recv,
+                      void* stream);
+
+/* The gradients of the attention calls (fp32) on their way to the projection: dq,
+ * dk_loc [T_q, ...] and dk_recv [T_r, Hkv, d] rotated back (the gradient through
+ * fc_rope_fwd and fc_kv_gather_rope, amplitude included), dv_loc and dv_recv as they
+ * are; each rounded to bf16 (out_bf16 != 0) or kept in fp32. One launch. Each may be
+ * NULL (not all); rope NULL rounds or copies only. */
+int fc_rope_bwd(fc_view view, const fc_rope* rope, int32_t out_bf16, const fc_rows* dq,
+                const fc_rows* dk_loc, const fc_rows* dv_loc, const fc_rows* dk_recv,
+                const fc_rows* dv_recv, void* stream);
 
 /* Forward. Writes o (bf16 [T_q,Hq,d]), optionally o_f32 (fp32, same shape;
  * NULL to skip) and lse (fp32 [Hq,T_q]). FC_TWO_PASS runs the local and the

@@ -15,6 +15,9 @@ view       a rank's view of a plan (its query tokens, the received KV set,
            document segments, pieces) and the tile maps derived from it.
 attention  document-masked causal attention forward/backward in fp64, its
            partial passes over a subset of keys, and the log-sum-exp merge.
+scores     the same with capped scores and a distance bias, and what an
+           implementation in bf16 and fp32 may be off by.
+rope       rotary positions, their gradient and their scaled frequencies.
 
 Parity status of each function is stated in its module header.
 """

@@ -22,10 +22,18 @@ SOURCES = [
     "host/view.cpp",
     "host/api.cpp",
     "host/noalloc.cpp",
+    "host/rope.cpp",
     "kernels/attn_fwd.hip",
+    "kernels/attn_fwd_cap.hip",
+    "kernels/attn_fwd_bias.hip",
+    "kernels/attn_fwd_cap_bias.hip",
     "kernels/attn_bwd.hip",
+    "kernels/attn_bwd_cap.hip",
+    "kernels/attn_bwd_bias.hip",
+    "kernels/attn_bwd_cap_bias.hip",
     "kernels/attn_bwd_dq.hip",
     "kernels/elementwise.hip",
+    "kernels/rope.hip",
 ]
 
 FLAGS = [

@@ -74,6 +74,23 @@ bool split_dq(const View& v, const void* ws, size_t ws_bytes) {
   return v.n_dq_slots && ws && ws_bytes >= pass_ws(v);
 }
 
+// A scored view's function for a kernel's parameters: cap_in takes a product to
+// twice its angle over the cap in log2 units, cap2 is the cap in those.
+template <class P>
+void set_score(P& p, const View& v, float scale) {
+  constexpr double kLog2e = 1.4426950408889634;
+  if (v.cap > 0) {
+    p.cap_in = float(2 * double(resolve_scale(scale, v.d)) * kLog2e / v.cap);
+    p.cap2 = float(v.cap * kLog2e);
+  }
+  if (!v.slopes.empty()) {
+    const float* m = reinterpret_cast<const float*>(v.dev_meta);
+    p.slopes = m + v.off.slopes;
+    p.q_pos = m + v.off.q_pos;
+    p.recv_pos = m + v.off.recv_pos;
+  }
+}
+
 fck::FwdParams fwd_params(const View& v, const int32_t* items, int64_t n,
                           const void* q, const void* k_loc, const void* v_loc, const void* k_recv,
                           const void* v_recv, float scale) {
@@ -91,6 +108,7 @@ fck::FwdParams fwd_params(const View& v, const int32_t* items, int64_t n,
   p.head_chunks = p.group / v.heads_per_tile;
   p.scale_log2 = resolve_scale(scale, v.d) * 1.4426950408889634f;
   p.t_q = v.t_q();
+  set_score(p, v, scale);
   return p;
 }
 
@@ -155,6 +173,7 @@ fck::BwdParams bwd_params(const View& v, const void* q, const void* k_loc, const
   p.dk_recv = dk_recv;
   p.dv_recv = dv_recv;
   p.t_q = v.t_q();
+  set_score(p, v, scale);
   return p;
 }
 
@@ -180,6 +199,7 @@ fck::DqParams dq_params(const View& v, const void* q, const void* k_loc, const v
   d.scale = resolve_scale(scale, v.d);
   d.dq = dq;
   d.t_q = v.t_q();
+  set_score(d, v, scale);
   return d;
 }
 

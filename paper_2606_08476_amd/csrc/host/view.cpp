@@ -19,6 +19,8 @@
 #include <hip/hip_runtime.h>
 
 #include <algorithm>
+#include <cmath>
+#include <cstring>
 #include <numeric>
 
 #include "internal.hpp"
@@ -453,6 +455,13 @@ int View::check_tables() const {
       return bad("forward combine entry", i);
   }
   if (bwd_qfirst.size() != bwd_launch.size() / 8 * size_t(bn_bwd / 32)) return bad("qfirst", 0);
+  const int32_t n_seg = int32_t(seg.size() / 4);
+  for (const auto* f : {&first_q, &first_r})
+    for (size_t i = 0; i < f->size(); ++i)
+      if (!(0 <= (*f)[i] && (*f)[i] < n_seg)) return bad("segment of a row", i);
+  // (the last segment ends with the last row: a walk over the ends stops there)
+  if (n_seg ? seg[4 * size_t(n_seg) - 4] != tq || seg[4 * size_t(n_seg) - 3] != tr : tq + tr > 0)
+    return bad("segment", size_t(n_seg));
   for (size_t i = 0; i < lim.size(); ++i)
     if (!(0 <= lim[i] && lim[i] <= tr)) return bad("receive limit", i);
   return FC_OK;
@@ -487,12 +496,27 @@ void View::build_meta() {
   off.dq_comb = put(dq_comb);
   off.fwd_units = put(fwd_units);
   off.fwd_comb = put(fwd_comb);
+  off.seg = put(seg);
+  off.first_q = put(first_q);
+  off.first_r = put(first_r);
+  if (!slopes.empty()) {
+    auto put_f = [&](const std::vector<float>& v) {
+      std::vector<int32_t> bits(v.size());
+      if (!v.empty()) std::memcpy(bits.data(), v.data(), v.size() * sizeof(float));
+      return put(bits);
+    };
+    std::vector<float> s2(slopes.size());
+    for (size_t h = 0; h < s2.size(); ++h) s2[h] = float(double(slopes[h]) * 1.4426950408889634);
+    off.slopes = put_f(s2);
+    off.q_pos = put_f(q_pos);
+    off.recv_pos = put_f(recv_pos);
+  }
   if (meta.empty()) meta.resize(64, 0);
 }
 
 int build_view(const int32_t* cu, int32_t n_docs, const fc_shard* shards, int64_t n_shards,
                int32_t cp, int32_t rank, int32_t hq, int32_t hkv, int32_t d,
-               const fc_tile_cfg* tiles, View& v) {
+               const fc_tile_cfg* tiles, const fc_score* score, View& v) {
   std::vector<int64_t> lens;
   if (int rc = doc_lengths(cu, n_docs, lens)) return rc;
   if (int rc = validate_plan(lens, cp, shards, n_shards, false)) return rc;
@@ -508,6 +532,21 @@ int build_view(const int32_t* cu, int32_t n_docs, const fc_shard* shards, int64_
   v.hq = hq;
   v.hkv = hkv;
   v.d = d;
+  if (score) {
+    if (!(score->cap == 0 || (score->cap >= FC_CAP_MIN && score->cap <= FC_CAP_MAX)))
+      return fail(FC_ERR_INVALID_ARG, "cap must be 0 or from FC_CAP_MIN to FC_CAP_MAX");
+    v.cap = score->cap;
+    if (score->slopes) {
+      for (int32_t h = 0; h < hq; ++h)
+        if (!(score->slopes[h] >= 0 && score->slopes[h] <= FC_SLOPE_MAX))
+          return fail(FC_ERR_INVALID_ARG, "slopes must be from 0 to FC_SLOPE_MAX");
+      // (distances are counted in fp32)
+      for (int64_t l : lens)
+        if (l > (int64_t(1) << 24))
+          return fail(FC_ERR_UNSUPPORTED, "a document of a view with slopes has more than 2^24 tokens");
+      v.slopes.assign(score->slopes, score->slopes + hq);
+    }
+  }
   // tile shapes: the forward / dQ query tile is 128 / (heads per workgroup)
   // rows, each of the 4 waves taking a quarter of them for every head; the
   // other shapes are compiled
@@ -568,6 +607,29 @@ int build_view(const int32_t* cu, int32_t n_docs, const fc_shard* shards, int64_
     const int64_t seg_len = v.q_cu[seg + 1] - v.q_cu[seg];
     v.pairs_loc += seg_len * (seg_len + 1) / 2;
   }
+  for (size_t s = 0; s < v.seg_doc.size(); ++s)
+    v.seg.insert(v.seg.end(), {v.q_cu[s + 1], v.recv_cu[s + 1], cu[v.seg_doc[s]], 0});
+  auto firsts = [&](int32_t n, int which) {
+    std::vector<int32_t> f;
+    for (int32_t t = 0, s = 0; t < n; t += 64) {
+      while (v.seg[4 * size_t(s) + which] <= t) ++s;
+      f.push_back(s);
+    }
+    return f;
+  };
+  v.first_q = firsts(v.t_q(), 0);
+  v.first_r = firsts(v.t_recv(), 1);
+  if (!v.slopes.empty()) {
+    // segments are in local order, and so are their received tokens
+    auto in_doc = [&](const std::vector<int32_t>& gpos, const std::vector<int32_t>& bounds) {
+      std::vector<float> p(gpos.size());
+      for (size_t s = 0; s < v.seg_doc.size(); ++s)
+        for (int32_t i = bounds[s]; i < bounds[s + 1]; ++i) p[i] = float(gpos[i] - cu[v.seg_doc[s]]);
+      return p;
+    };
+    v.q_pos = in_doc(v.q_gpos, v.q_cu);
+    v.recv_pos = in_doc(v.recv_gpos, v.recv_cu);
+  }
   v.build_tiles();
   if (int rc = v.check_tables()) return rc;
   v.build_meta();
@@ -580,18 +642,36 @@ using namespace fc;
 
 extern "C" {
 
-int fc_view_create(const int32_t* cu, int32_t n_docs, const fc_shard* shards, int64_t n_shards,
-                   int32_t cp, int32_t rank, int32_t hq, int32_t hkv, int32_t d,
-                   const fc_tile_cfg* tiles, fc_view* out) {
+int fc_view_create_scored(const int32_t* cu, int32_t n_docs, const fc_shard* shards,
+                          int64_t n_shards, int32_t cp, int32_t rank, int32_t hq, int32_t hkv,
+                          int32_t d, const fc_tile_cfg* tiles, const fc_score* score, fc_view* out) {
   clear_error();
   if (!out) return fail(FC_ERR_INVALID_ARG, "out is null");
   *out = nullptr;
   View* v = new View();
-  if (int rc = build_view(cu, n_docs, shards, n_shards, cp, rank, hq, hkv, d, tiles, *v)) {
+  if (int rc = build_view(cu, n_docs, shards, n_shards, cp, rank, hq, hkv, d, tiles, score, *v)) {
     delete v;
     return rc;
   }
   *out = reinterpret_cast<fc_view>(v);
+  return FC_OK;
+}
+
+int fc_view_create(const int32_t* cu, int32_t n_docs, const fc_shard* shards, int64_t n_shards,
+                   int32_t cp, int32_t rank, int32_t hq, int32_t hkv, int32_t d,
+                   const fc_tile_cfg* tiles, fc_view* out) {
+  return fc_view_create_scored(cu, n_docs, shards, n_shards, cp, rank, hq, hkv, d, tiles, nullptr,
+                               out);
+}
+
+int fc_view_get_score(fc_view view, float* cap, int32_t* biased, float* slopes) {
+  clear_error();
+  if (!view) return fail(FC_ERR_INVALID_ARG, "view is null");
+  const View& v = *reinterpret_cast<View*>(view);
+  if (cap) *cap = v.cap;
+  if (biased) *biased = !v.slopes.empty();
+  if (slopes)
+    for (int32_t h = 0; h < v.hq; ++h) slopes[h] = v.slopes.empty() ? 0.f : v.slopes[h];
   return FC_OK;
 }
 

@@ -14,10 +14,18 @@ struct View {
   int32_t hq = 0, hkv = 0, d = 0, heads_per_tile = 1;
   int32_t bm_fwd = 0, bn_fwd = 0, bm_bwd = 0, bn_bwd = 0;
 
+  // score function: cap (0: none) and slopes per query head (empty: none), as given
+  float cap = 0;
+  std::vector<float> slopes;
+
   std::vector<int32_t> q_gpos, recv_gpos;   // global positions, local / receive order
+  std::vector<float> q_pos, recv_pos;       // with slopes: positions in the document
   std::vector<int32_t> seg_doc, q_cu, recv_cu, seg_piece;
   std::vector<int32_t> pieces;              // 5 per piece: seg, q_start, q_end, g_start, n_P
   std::vector<int32_t> lim;                 // receive index end seen by each query
+  // where tokens' documents start, for rotary positions: 4 per segment (local end,
+  // received end, document start, 0), and the segment of every 64th token
+  std::vector<int32_t> seg, first_q, first_r;
   int64_t pairs_loc = 0, pairs_recv = 0;
 
   // work lists, 8 int32 per item (layout documented in flashcp.h), in map
@@ -58,6 +66,8 @@ struct View {
     int64_t bwd_launch, bwd_reduce, bwd_qfirst;
     int64_t dq_items, dq_comb;
     int64_t fwd_units, fwd_comb;
+    int64_t seg, first_q, first_r;
+    int64_t slopes, q_pos, recv_pos;        // with slopes only; fp32, slopes in log2 units
   } off{};
   const int32_t* dev_meta = nullptr;        // set by fc_view_bind
   // a split view's own slots, behind the tables in the bound buffer (null: the
@@ -100,6 +110,6 @@ struct View {
 
 int build_view(const int32_t* cu, int32_t n_docs, const fc_shard* shards, int64_t n_shards,
                int32_t cp, int32_t rank, int32_t hq, int32_t hkv, int32_t d,
-               const fc_tile_cfg* tiles, View& v);
+               const fc_tile_cfg* tiles, const fc_score* score, View& v);
 
 }  // namespace fc

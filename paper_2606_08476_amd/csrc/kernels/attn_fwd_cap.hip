@@ -1,0 +1,9 @@
+// Forward attention with capped scores (gfx950); the per-workgroup body is in
+// fwd.hpp.
+#include "fwd.hpp"
+
+namespace fck {
+
+template hipError_t launch_fwd_sc<kScoreCap>(const FwdParams&, int, int, int, hipStream_t);
+
+}  // namespace fck

@@ -30,18 +30,33 @@
 // reads) and adds it into dQ with fp32 atomics. No second pass recomputes S
 // and dP; the order of the additions into dQ, and so its last bits, varies
 // from run to run.
+//
+// Scored views (SC, see score.hpp): S becomes the score before the exponential, the
+// bias from the row's position and slope, which go through LDS as its LSE does.
+// With a cap dS has the factor 1 - tanh^2 = 4 (r - r^2): r - r^2 is kept beside P, as
+// fp16 (2^-11 of it, a quarter of what dS's own rounding to bf16 may be off by;
+// sixteen fp32 registers more would spill), until P has been packed for dV; then W =
+// P (r - r^2) takes P's place in dS = W (dP - D), and the 4 is in the final scale.
+// P's residual is formed before that, where it is needed.
 #include "common.hpp"
 #include "launch.hpp"
+#include "score.hpp"
 
 #include <type_traits>
 
 namespace fck {
 
-template <int D, bool DQ = false>
+template <int D, bool DQ = false, int SC = 0>
 struct DkdvLds {
-  // -LSE/-delta/limit slots, the key tile, two Q and two dO tiles; with DQ the
-  // transposed dS tile (128 keys x 32 queries, bf16) after them
-  static constexpr uint32_t bytes = 6 * 256 + (128 + 4 * 32) * D * 2 + (DQ ? 128 * 32 * 2 : 0);
+  // -LSE/-delta/limit slots (and the rows' positions), the key tile, two
+  // Q and two dO tiles; with DQ the transposed dS tile (128 keys x 32 queries,
+  // bf16) after them
+  static constexpr uint32_t stats = (SC & kScoreBias) ? 4 * 256 : 3 * 256;  // per buffer
+  // with DQ and a cap, at head dim 128, a sixteenth of each wave's V operands, whose
+  // registers would spill
+  static constexpr bool vpart = DQ && (SC & kScoreCap) && D == 128;
+  static constexpr uint32_t bytes = 2 * stats + (128 + 4 * 32) * D * 2 + (DQ ? 128 * 32 * 2 : 0) +
+                                    (vpart ? 4 * 1024 : 0);
 };
 
 // What the residual branch has kept of the bf16 roundings it subtracts.
@@ -49,8 +64,9 @@ enum { kKeepNone = 0, kKeepDs = 1, kKeepAll = 2 };
 
 // One workgroup's key tile (workgroup index b); smem: DkdvLds<D, DQ>::bytes
 // of shared memory. HPI (1, 2 or 4) must divide the group size.
-template <int D, bool DQ, int HPI, int KEEP>
+template <int D, bool DQ, int HPI, int KEEP, int SC = 0>
 __device__ __forceinline__ void dkdv_tile(const BwdParams& p, int b, char* smem) {
+  constexpr bool CAP = SC & kScoreCap, BIAS = SC & kScoreBias;
   constexpr int BN = 128;       // keys per workgroup
   constexpr int BM = 32;        // (query row, head) pairs per iteration
   constexpr int RPI = BM / HPI; // query rows per iteration and head
@@ -59,12 +75,14 @@ __device__ __forceinline__ void dkdv_tile(const BwdParams& p, int b, char* smem)
   constexpr int DB = D / 32;
   constexpr uint32_t KT = BN * D * 2;  // bytes of the key tile
   constexpr uint32_t QT = BM * D * 2;  // bytes of a Q or dO tile
-  // LDS layout (bytes): per buffer b, -LSE in log2 units at 256*3b, -delta at
-  // +256, receive limits at +512 (one wave each, the first BM entries used); then
+  // LDS layout (bytes): per buffer b, -LSE in log2 units at ST*b, -delta at
+  // +256, receive limits at +512 (one wave each, the first BM entries used), with a
+  // bias the rows' positions at +768; then
   // the key tile; then Q and dO of buffer 0 and of buffer 1. The loop is
   // unrolled by two, so every read names its buffer with a compile-time
   // offset (all below 64 KiB, the reach of the offset field).
-  constexpr uint32_t OK = 6 * 256;
+  constexpr uint32_t ST = DkdvLds<D, DQ, SC>::stats;
+  constexpr uint32_t OK = 2 * ST;
   constexpr uint32_t OQ0 = OK + KT, OO0 = OQ0 + QT, OQ1 = OO0 + QT, OO1 = OQ1 + QT;
   // dS^T tile (DQ only): row k (key) holds the tile's 32 queries, 64 bytes;
   // the 8-byte chunk c (queries 4c..4c+3) of row k sits at chunk position
@@ -72,9 +90,13 @@ __device__ __forceinline__ void dkdv_tile(const BwdParams& p, int b, char* smem)
   // chunk) and the transpose reads (4 keys x 16 queries per 16 lanes) both
   // spread over the 64 banks
   constexpr uint32_t ODS = OO1 + QT;
-  static_assert(ODS + (DQ ? 128 * 32 * 2 : 0) == DkdvLds<D, DQ>::bytes, "LDS layout");
+  constexpr bool VPART = DkdvLds<D, DQ, SC>::vpart;  // V's first k-step is read from LDS
+  constexpr uint32_t OVP = ODS + 128 * 32 * 2;
+  static_assert(ODS + (DQ ? 128 * 32 * 2 : 0) + (VPART ? 4096 : 0) == DkdvLds<D, DQ, SC>::bytes, "LDS layout");
 
   const int lane = threadIdx.x & 63, wave = wave_id();
+  // the lane's index where it should not be held in a register up to here
+  auto lane_here = [&]() { return SC ? fresh_lane() : opaque(uint32_t(lane)); };
   const int half = lane >> 5;
   const int kvh = b % p.hkv;
   const int item = b / p.hkv;  // the launch list is in launch order
@@ -129,7 +151,13 @@ __device__ __forceinline__ void dkdv_tile(const BwdParams& p, int b, char* smem)
   // most (backward of a 16K sequence, 32/8 heads, 1014 -> 1003 us where two runs
   // differ by 5): issue slots are not what is short.
   float row_stat = 0.f;
-  const TileLoader<D, BM, 256, RPI> ldq(p.hq * D, D);
+  // SC: cap2 goes with the rows' -LSE (put_rows)
+  const float sl2 = CAP ? p.cap_in : p.scale * kLog2e, cap2 = p.cap2;
+  const float gscale = CAP ? 4.f * p.scale : p.scale;  // (W leaves out a 4)
+  // position of this lane's key
+  const float* const kposg = src ? p.recv_pos : p.q_pos;
+  const float kpos = BIAS ? kposg[min(k0 + 32 * wave + (lane & 31), k1 - 1)] : 0.f;
+  const TileLoader<D, BM, 256, RPI, SC == 0 ? 0 : DQ && D == 128 ? 2 : 1> ldq(p.hq * D, D);
   auto fetch = [&](int hh, int tt, int buf) {
     const int h = kvh * p.group + hh * HPI;
     const int t0 = q0 + tt * RPI;
@@ -137,21 +165,22 @@ __device__ __forceinline__ void dkdv_tile(const BwdParams& p, int b, char* smem)
     const uint32_t sb = lds_addr(smem);
     ldq.load_at(sb + (buf ? OQ1 : OQ0), p.q + base, q1 - t0);
     ldq.load_at(sb + (buf ? OO1 : OO0), p.dout + base, q1 - t0);
-    const int m = lane & 31;
+    const int m = (SC ? int(fresh_lane()) : lane) & 31;
     const uint32_t roff = 4u * uint32_t(min(t0 + m % RPI, q1 - 1));
     const uint32_t qoff = roff + 4u * uint32_t(m / RPI) * uint32_t(p.t_q);
-    const uint32_t sm = sb + 768u * buf;
+    const uint32_t sm = sb + ST * buf;
     if (wave < 2) {
       const float* const rows = (wave == 0 ? p.lse : p.delta) + (size_t)h * p.t_q;
       row_stat = *reinterpret_cast<const float*>(reinterpret_cast<const char*>(rows) + qoff);
     } else if (wave == 2 && src) {
       lds_copy4(p.lim, roff, sm + 512);
     }
+    if (BIAS && wave == 3) lds_copy4(p.q_pos, roff, sm + 768);
   };
   auto put_rows = [&](int buf) {
     if (wave < 2)
-      *reinterpret_cast<float*>(smem + 768 * buf + 256 * wave + 4 * opaque(uint32_t(lane))) =
-          wave == 0 ? -row_stat * kLog2e : -row_stat;
+      *reinterpret_cast<float*>(smem + ST * buf + 256 * wave + 4 * lane_here()) =
+          wave == 0 ? (CAP ? __builtin_fmaf(-row_stat, kLog2e, cap2) : -row_stat * kLog2e) : -row_stat;
   };
 
   // per-lane LDS byte offsets (swizzled tiles): row reads of a 32-row block
@@ -168,7 +197,6 @@ __device__ __forceinline__ void dkdv_tile(const BwdParams& p, int b, char* smem)
     dv[db] = zero16();
   }
   const bool kfull = k1 - k0 == BN;
-  const float sl2 = p.scale * kLog2e;
 
   wait_async();
   __syncthreads();
@@ -176,6 +204,7 @@ __device__ __forceinline__ void dkdv_tile(const BwdParams& p, int b, char* smem)
     const int vb = row_base<D>(32 * wave, lane);
 #pragma unroll
     for (int ks = 0; ks < KS; ++ks) vreg[ks] = lds_b128(smem, 2u * uint32_t(vb ^ (ks << 4)), OQ0);
+    if (VPART) *reinterpret_cast<bf16x8*>(smem + OVP + 1024 * wave + 16 * lane) = vreg[0];
   }
   __syncthreads();  // every wave holds its V rows before the Q/dO copies
   if (n_it > 0) {
@@ -205,16 +234,16 @@ __device__ __forceinline__ void dkdv_tile(const BwdParams& p, int b, char* smem)
   // (the lane-derived addresses of the dQ stage are recomputed from an
   // opaque copy of the lane index, not hoisted and held across the loop)
   auto put_ds = [&](const uint4& w0, const uint4& w1) {
-    const uint32_t krow = 32 * wave + (opaque(uint32_t(lane)) & 31);
+    const uint32_t krow = 32 * wave + (lane_here() & 31);
     const uint32_t row = ODS + krow * 64, sw = (krow >> 2) & 7;
     *reinterpret_cast<uint2*>(smem + row + 8 * (uint32_t(half) ^ sw)) = make_uint2(w0.x, w0.y);
     *reinterpret_cast<uint2*>(smem + row + 8 * ((2u + half) ^ sw)) = make_uint2(w0.z, w0.w);
     *reinterpret_cast<uint2*>(smem + row + 8 * ((4u + half) ^ sw)) = make_uint2(w1.x, w1.y);
     *reinterpret_cast<uint2*>(smem + row + 8 * ((6u + half) ^ sw)) = make_uint2(w1.z, w1.w);
   };
-  auto tile = [&](int t0, auto bufc, bool edge) {
+  auto tile = [&](int t0, int hh, auto bufc, bool edge) {
     constexpr int B = decltype(bufc)::value;
-    constexpr uint32_t QO = B ? OQ1 : OQ0, OO = B ? OO1 : OO0, SO = 768u * B;
+    constexpr uint32_t QO = B ? OQ1 : OQ0, OO = B ? OO1 : OO0, SO = ST * B;
     // masks: this lane's key against query rows t0 + 4*half + cq, cq =
     // (8g) % RPI + j (register 4g + j, pair 8g + 4*half + j): rows cq < hiq
     // exist; on a local diagonal the key is
@@ -223,16 +252,25 @@ __device__ __forceinline__ void dkdv_tile(const BwdParams& p, int b, char* smem)
     // (this lane's key is recomputed here from an opaque lane index rather
     // than held across the loop)
     const bool diag = t0 < qfull;
-    const uint32_t ln = opaque(uint32_t(lane));
-    const int hf = int(ln >> 5);
+    const uint32_t ln = lane_here();
+    const int hf = int(ln >> 5), hrow = SC ? hf : half;
     const int kid = k0 + 32 * wave + int(ln & 31);
     const bool kval = kid < k1;
     const int hiq = q1 - t0 - 4 * hf;
     const int lo = !kval ? 0x40000000 : (diag && !src) ? kid - t0 - 4 * hf : -0x40000000;
     const int kl = (diag && src) ? (kval ? kid : 0x7fffffff) : -0x7fffffff;
 
+    // BIAS: the slopes of the iteration's heads (wave-uniform: row 8g + ... of the
+    // iteration is of head 8g / RPI)
+    float slope2[HPI];
+#pragma unroll
+    for (int i = 0; i < HPI; ++i) slope2[i] = BIAS ? p.slopes[kvh * p.group + hh * HPI + i] : 0.f;
+
     f32x16 sacc = zero16(), dpacc;
-    bf16x8 ra[3], rb[3], pa[2], sa[2];
+    typedef _Float16 f16x2 __attribute__((ext_vector_type(2)));
+    f16x2 rr[8];  // CAP: r - r^2
+    float r1 = 0.f;
+    bf16x8 ra[3], rb[3], pa[2], sa[2], plo[2];
     // Where P is large (short documents, keys near the diagonal) the bf16
     // rounding of P and dS dominates the dV/dK error. On a wave's tile with
     // any P above 1/16 (rare on long documents) the bf16 residuals of P and
@@ -264,7 +302,9 @@ __device__ __forceinline__ void dkdv_tile(const BwdParams& p, int b, char* smem)
       f32x16 pf = pv, sf = sv;
       if constexpr (KEEP < kKeepAll) asm volatile("" : "+v"(pf));
       if constexpr (KEEP < kKeepDs) asm volatile("" : "+v"(sf));
-      auto p_lo = [&](int i) { return KEEP < kKeepAll ? lo8(pf, 8 * i) : lo8(pf, 8 * i, pk[i]); };
+      auto p_lo = [&](int i) {
+        return CAP ? plo[i] : KEEP < kKeepAll ? lo8(pf, 8 * i) : lo8(pf, 8 * i, pk[i]);
+      };
       auto s_lo = [&](int i) { return KEEP < kKeepDs ? lo8(sf, 8 * i) : lo8(sf, 8 * i, sk[i]); };
       bf16x8 lo[2];
       rd(0);
@@ -287,6 +327,9 @@ __device__ __forceinline__ void dkdv_tile(const BwdParams& p, int b, char* smem)
       });
     };
     f32x4 l4[4];
+    // SC: -LSE (and positions) of the rows of a slot's exponentials, by slot
+    typedef float rowv __attribute__((ext_vector_type(EP)));
+    rowv le[2], ce[2];
     // P = 0 where the key is not seen: keys past the range, later keys on a
     // local diagonal, keys at or past a row's receive limit on a received
     // diagonal (edge tiles only)
@@ -294,7 +337,7 @@ __device__ __forceinline__ void dkdv_tile(const BwdParams& p, int b, char* smem)
       int4 m4[4];
 #pragma unroll
       for (int g = 0; g < 4; ++g)
-        m4[g] = *reinterpret_cast<const int4*>(smem + SO + 512 + 4 * (8 * g + 4 * half));
+        m4[g] = *reinterpret_cast<const int4*>(smem + SO + 512 + 4 * (8 * g + 4 * hrow));
 #pragma unroll
       for (int e = 0; e < 16; ++e) {
         const int g = e >> 2, j = e & 3, cq = (8 * g) % RPI + j;
@@ -314,6 +357,8 @@ __device__ __forceinline__ void dkdv_tile(const BwdParams& p, int b, char* smem)
         rb[n % 3] = lds_b128(smem, r + kofs, 0);
       } else if (n < 2 * KS) {
         a = lds_b128(smem, pr ^ ((n - KS) << 5), OO);
+        // (what its own wave has stored)
+        if (VPART && n == KS) rb[n % 3] = lds_b128(smem, OVP + 1024 * wave + 16 * ln, 0);
       } else {
         const int u = n < 2 * KS + 2 * DB ? n - 2 * KS : n - 2 * KS - 2 * DB;
         const int kh = u / DB, db = u % DB;
@@ -331,23 +376,40 @@ __device__ __forceinline__ void dkdv_tile(const BwdParams& p, int b, char* smem)
       // first slot that uses them
 #pragma unroll
       for (int g = 0; g < 4; ++g) {
-        if (KS + 4 * g / EP == n + 2)
-          l4[g] = *reinterpret_cast<const f32x4*>(smem + SO + 4 * (8 * g + 4 * half));
+        if (!SC && KS + 4 * g / EP == n + 2)
+          l4[g] = *reinterpret_cast<const f32x4*>(smem + SO + 4 * (8 * g + 4 * hrow));
         if (KS == n + 2) {
-          const f32x4 d4 = *reinterpret_cast<const f32x4*>(smem + SO + 256 + 4 * (8 * g + 4 * half));
+          const f32x4 d4 = *reinterpret_cast<const f32x4*>(smem + SO + 256 + 4 * (8 * g + 4 * hrow));
 #pragma unroll
           for (int j = 0; j < 4; ++j) dpacc[4 * g + j] = d4[j];
         }
+      }
+      if (SC && n + 1 >= KS && n + 1 < 2 * KS) {
+        const int e = (n + 1 - KS) * EP, ro = 4 * (8 * (e / 4) + e % 4);
+        le[n % 2] = *reinterpret_cast<const rowv*>(smem + SO + ro + 16 * hrow);
+        if (BIAS) ce[n % 2] = *reinterpret_cast<const rowv*>(smem + SO + 768 + ro + 16 * hrow);
       }
       const bf16x8& a = ra[n % 3];
       if (n < KS) {
         sacc = mfma32(a, rb[n % 3], sacc);
       } else if (n < 2 * KS) {
-        dpacc = mfma32(a, vreg[n - KS], dpacc);
+        dpacc = mfma32(a, VPART && n == KS ? rb[n % 3] : vreg[n - KS], dpacc);
 #pragma unroll
         for (int e = (n - KS) * EP; e < (n - KS + 1) * EP; ++e) {
           const int g = e >> 2, j = e & 3;
-          sacc[e] = __builtin_amdgcn_exp2f(__builtin_fmaf(sacc[e], sl2, l4[g][j]));
+          float off = SC ? le[(n - 1) & 1][e % EP] : l4[g][j];
+          if constexpr (BIAS) off = __builtin_fmaf(slope2[8 * g / RPI], kpos - ce[(n - 1) & 1][e % EP], off);
+          if constexpr (CAP) {
+            const float r = cap_r(sacc[e], sl2);
+            sacc[e] = __builtin_amdgcn_exp2f(__builtin_fmaf(r, -2.f * cap2, off));
+            const float r2 = __builtin_fmaf(-r, r, r);
+            if (e & 1)
+              rr[e / 2] = f16x2{(_Float16)r1, (_Float16)r2};
+            else
+              r1 = r2;
+          } else {
+            sacc[e] = __builtin_amdgcn_exp2f(__builtin_fmaf(sacc[e], sl2, off));
+          }
         }
         if ((n - KS + 1) * EP == 8) pa[0] = pack8(sacc, 0);
         if (n == 2 * KS - 1) {
@@ -360,6 +422,14 @@ __device__ __forceinline__ void dkdv_tile(const BwdParams& p, int b, char* smem)
 #pragma unroll
           for (int e = 1; e < 16; ++e) pmax = fmaxf(pmax, sacc[e]);
           split = __any(pmax > kSplitP);
+          if constexpr (CAP) {
+            if (split) {
+              plo[0] = lo8(sacc, 0, pa[0]);
+              plo[1] = lo8(sacc, 8, pa[1]);
+            }
+#pragma unroll
+            for (int e = 0; e < 16; ++e) sacc[e] *= (float)rr[e / 2][e & 1];
+          }
         }
       } else if (n < 2 * KS + 2 * DB) {
         const int u = n - 2 * KS, kh = u / DB, db = u % DB;
@@ -396,7 +466,7 @@ __device__ __forceinline__ void dkdv_tile(const BwdParams& p, int b, char* smem)
   auto dq_part = [&](f32x16& qacc) {
     __syncthreads();
     const int cb = wave % DB, kpart = wave / DB;
-    const uint32_t ln = opaque(uint32_t(lane));
+    const uint32_t ln = lane_here();
     const int t = ln & 15, g = (ln >> 4) & 1, hf = ln >> 5;
     // (a key part starts at a multiple of 64 rows: its offset leaves the
     // low bits the XORs act on untouched)
@@ -432,7 +502,7 @@ __device__ __forceinline__ void dkdv_tile(const BwdParams& p, int b, char* smem)
   // comes an iteration later) instead of stalling this one.
   auto dq_add = [&](int t0, int hh, const f32x16& qacc) {
     const int cb = wave % DB;
-    const uint32_t ln = opaque(uint32_t(lane));
+    const uint32_t ln = lane_here();
     const int hf = ln >> 5;
     // C layout: register i is pair 8*(i/4) + 4h + i%4 (query row
     // (8*(i/4)) % RPI + 4h + i%4 of head set member (8*(i/4)) / RPI), column
@@ -451,7 +521,7 @@ __device__ __forceinline__ void dkdv_tile(const BwdParams& p, int b, char* smem)
     for (int i = 0; i < 16; ++i) {
       const int r0 = (8 * (i >> 2)) % RPI + (i & 3), hm = (8 * (i >> 2)) / RPI;
       float* const bi = base + size_t(r0) * rs + hm * D;
-      if (t0 + r0 + 4 * hf < q1) atomicAdd(bi + loff, p.scale * qacc[i]);
+      if (t0 + r0 + 4 * hf < q1) atomicAdd(bi + loff, gscale * qacc[i]);
     }
   };
   // One pipelined iteration: start the next tile's copies, compute this one,
@@ -470,7 +540,7 @@ __device__ __forceinline__ void dkdv_tile(const BwdParams& p, int b, char* smem)
     pt = opaque(pt);
     const int tlast = min(t0 + RPI, q1) - 1;
     const bool computed = !(kw >= k1 || tlast < qfirst);
-    if (computed) tile(t0, bufc, !(t0 >= qfull && t0 + RPI <= q1 && kw + 32 <= k1));
+    if (computed) tile(t0, hh, bufc, !(t0 >= qfull && t0 + RPI <= q1 && kw + 32 <= k1));
     f32x16 qacc;
     if constexpr (DQ) {
       if (!computed) put_ds(uint4{0u, 0u, 0u, 0u}, uint4{0u, 0u, 0u, 0u});
@@ -499,14 +569,15 @@ __device__ __forceinline__ void dkdv_tile(const BwdParams& p, int b, char* smem)
     base = (size_t(slot) * p.hkv + kvh) * BN * D;
     r0 = 0;
   }
+  const int le = SC ? int(fresh_lane()) : lane;
 #pragma unroll
   for (int db = 0; db < DB; ++db) {
 #pragma unroll
     for (int i = 0; i < 16; ++i) {
-      const int r = 32 * wave + 8 * (i >> 2) + 4 * half + (i & 3);
+      const int r = 32 * wave + 8 * (i >> 2) + 4 * (SC ? le >> 5 : half) + (i & 3);
       if (k0 + r < k1) {
-        const size_t g = base + size_t(r0 + r) * rs + 32 * db + (lane & 31);
-        outK[g] = p.scale * dk[db][i];
+        const size_t g = base + size_t(r0 + r) * rs + 32 * db + ((SC ? le : lane) & 31);
+        outK[g] = gscale * dk[db][i];
         outV[g] = dv[db][i];
       }
     }

@@ -15,22 +15,30 @@
 // here costs two extra products per key tile compared with accumulating dQ
 // inside the key-major kernel, but removes that kernel's dQ traffic and
 // frees the registers and LDS that limit its occupancy.
+//
+// Scored views (SC, see score.hpp): S becomes the score before the exponential; with
+// a cap, P (r - r^2) takes P's place in dS (its 4 is in the final scale), which
+// needs no register more. A bias takes the keys' positions from LDS, copied per
+// tile by the first wave.
 #include "common.hpp"
 #include "launch.hpp"
+#include "score.hpp"
 
 #include <type_traits>
 
 namespace fck {
 
-template <int D>
+template <int D, int SC = 0>
 struct DqLds {
-  static constexpr uint32_t bytes = 4 * 64 * D * 2;
+  // two K and two V tiles; with a bias the positions of two tiles' keys
+  static constexpr uint32_t bytes = 4 * 64 * D * 2 + ((SC & kScoreBias) ? 2 * 256 : 0);
 };
 
 // One workgroup's query tile (workgroup index b); smem: DqLds<D>::bytes of
 // shared memory. HOLD: sixteen registers hold -D for dP's accumulators.
-template <int D, int HPW, bool HOLD>
+template <int D, int HPW, bool HOLD, int SC = 0>
 __device__ __forceinline__ void dq_tile(const DqParams& p, int b, char* smem) {
+  constexpr bool CAP = SC & kScoreCap, BIAS = SC & kScoreBias;
   constexpr int BN = 64;
   constexpr int RPW = 32 / HPW;  // query rows per wave and head
   constexpr int KS = D / 16;
@@ -38,7 +46,8 @@ __device__ __forceinline__ void dq_tile(const DqParams& p, int b, char* smem) {
   constexpr uint32_t TILE = BN * D * 2;  // bytes of one K or V tile
   // LDS: K0 | V0 | K1 | V1 (double buffer); the loop is unrolled by two so
   // every read names its buffer with a compile-time offset
-  static_assert(4 * TILE == DqLds<D>::bytes, "LDS layout");
+  constexpr uint32_t OP = 4 * TILE;  // BIAS: key positions
+  static_assert(OP + (BIAS ? 512 : 0) == DqLds<D, SC>::bytes, "LDS layout");
 
   const int lane = threadIdx.x & 63, wave = wave_id();
   const int half = lane >> 5;
@@ -56,12 +65,13 @@ __device__ __forceinline__ void dq_tile(const DqParams& p, int b, char* smem) {
   const int qrow = q0 + wave * RPW + l31 % RPW;
   const bool qvalid = qrow < q1;
   const bool active = q0 + wave * RPW < q1;  // wave-uniform
-  const float sl2 = p.scale * kLog2e;
+  const float sl2 = CAP ? p.cap_in : p.scale * kLog2e;
+  const float gscale = CAP ? 4.f * p.scale : p.scale;
 
   const int n_r = (r1 - r0 + BN - 1) / BN;
   const int n_t = n_r + (l1 - l0 + BN - 1) / BN;
 
-  const TileLoader<D, BN> ld(p.hkv * D);
+  const TileLoader<D, BN, 256, BN, SC != 0> ld(p.hkv * D);
   auto fetch = [&](int j, uint32_t kofs) {
     const bool rs = j < n_r;
     const int k0 = rs ? r0 + j * BN : l0 + (j - n_r) * BN;
@@ -69,7 +79,14 @@ __device__ __forceinline__ void dq_tile(const DqParams& p, int b, char* smem) {
     const size_t base = (size_t(k0) * p.hkv + kvh) * D;
     ld.load_at(lds_addr(smem) + kofs, (rs ? p.k_recv : p.k_loc) + base, hi - k0);
     ld.load_at(lds_addr(smem) + kofs + TILE, (rs ? p.v_recv : p.v_loc) + base, hi - k0);
+    if (BIAS && wave == 0) {  // and the keys' positions, a key per lane
+      const float* pos = rs ? p.recv_pos : p.q_pos;
+      lds_copy4(pos + k0, 4u * uint32_t(min(int(fresh_lane()), hi - k0 - 1)),
+                lds_addr(smem) + OP + kofs / (2 * TILE / 256));
+    }
   };
+
+  const float cap2 = p.cap2, slope2 = BIAS ? p.slopes[h] : 0.f;
 
   // the workgroup's Q and dO rows through LDS first (Q over the second K/V
   // buffer, dO over the first), then key tile 0
@@ -82,6 +99,14 @@ __device__ __forceinline__ void dq_tile(const DqParams& p, int b, char* smem) {
   if (qvalid) {
     lse2 = p.lse[(size_t)h * p.t_q + qrow] * kLog2e;
     ndel = -p.delta[(size_t)h * p.t_q + qrow];
+  }
+  // SC: the row's share of its scores less its LSE; what rounding it left out scales
+  // every P of the row alike, and so its dQ
+  // (row_scale, from values read again: not held across the loop)
+  float off2 = CAP ? cap2 - lse2 : -lse2;
+  if constexpr (BIAS) {
+    float rest;
+    off2 = row_offset(off2, slope2, p.q_pos[min(qrow, q1 - 1)], rest);
   }
 
   // per-lane LDS byte offsets: K/V rows for k-step ks, and the two transpose
@@ -145,7 +170,9 @@ __device__ __forceinline__ void dq_tile(const DqParams& p, int b, char* smem) {
       // give P = 0. Only edge tiles (diagonal, or running past the range)
       // mask, in one branch before each half's dS.
       const bool diag = !rs && k0 >= ldiag;
-      const int rel = (diag ? min(hi, qrow + 1) : hi) - k0 - 4 * half;
+      const int ln = SC ? int(fresh_lane()) : lane, hf = SC ? ln >> 5 : half;
+      const int qr = SC ? q0 + wave * RPW + (ln & 31) % RPW : qrow;
+      const int rel = (diag ? min(hi, qr + 1) : hi) - k0 - 4 * hf;
       const bool edge = diag || k0 + BN > hi;
 
       f32x16 s[2] = {zero16(), zero16()}, dp[2];
@@ -161,8 +188,26 @@ __device__ __forceinline__ void dq_tile(const DqParams& p, int b, char* smem) {
           a = cat8(lds_tr(smem, pt[db][0], ro), lds_tr(smem, pt[db][1], ro));
         }
       };
+      // BIAS: positions of the EP keys of a slot's exponentials, read a slot ahead
+      typedef float posv __attribute__((ext_vector_type(EP)));
+      posv kp[2];
+      auto rd_pos = [&](int t) {
+        const int e = t % KS * EP;
+        if (BIAS && t >= 0 && t < 2 * KS)
+          kp[t & 1] = *reinterpret_cast<const posv*>(
+              smem + OP + decltype(buf)::value * 256 + 16 * hf +
+              4 * (32 * (t / KS) + 8 * (e / 4) + e % 4));
+      };
       auto pexp = [&](int mb, int i) {
-        s[mb][i] = __builtin_amdgcn_exp2f(__builtin_fmaf(s[mb][i], sl2, -lse2));
+        float off = off2;
+        if constexpr (BIAS) off = __builtin_fmaf(slope2, kp[(mb * KS + i / EP) & 1][i % EP], off);
+        if constexpr (CAP) {
+          const float r = cap_r(s[mb][i], sl2);
+          s[mb][i] = __builtin_amdgcn_exp2f(__builtin_fmaf(r, -2.f * cap2, off)) *
+                     __builtin_fmaf(-r, r, r);
+        } else {
+          s[mb][i] = __builtin_amdgcn_exp2f(__builtin_fmaf(s[mb][i], sl2, off));
+        }
       };
       auto mask = [&](int mb) {
         if (edge) {
@@ -205,6 +250,7 @@ __device__ __forceinline__ void dq_tile(const DqParams& p, int b, char* smem) {
       static_for<0, NS>([&](auto nc) {
         constexpr int n = decltype(nc)::value;
         if (n + 2 < NS) rd(n + 2);
+        rd_pos(n + 1 - KS);
         const bf16x8& a = ring[n % 3];
         if (n < 2 * KS) {
           const int ks = n % KS, mb = n / KS;
@@ -250,6 +296,17 @@ __device__ __forceinline__ void dq_tile(const DqParams& p, int b, char* smem) {
     if (j + 1 < n_t) step(j + 1, std::integral_constant<int, 1>());
   }
 
+  auto row_scale = [&](float f) {
+    if constexpr (BIAS) {
+      const int l = int(opaque(uint32_t(lane)) & 31), r = min(q0 + wave * RPW + l % RPW, q1 - 1);
+      const int hh = kvh * p.group + hc * HPW + l / RPW;
+      const float l2 = p.lse[(size_t)hh * p.t_q + r] * kLog2e;
+      float rest;
+      row_offset(CAP ? cap2 - l2 : -l2, p.slopes[hh], p.q_pos[r], rest);
+      f *= __builtin_amdgcn_exp2f(rest);
+    }
+    return f;
+  };
   // a part of a split key range: the unscaled sums go to the part's slot, in
   // register order (1 KiB per store instruction), and are added up by
   // dq_combine_kernel
@@ -257,13 +314,14 @@ __device__ __forceinline__ void dq_tile(const DqParams& p, int b, char* smem) {
     if (active) {
       const size_t slot = (size_t(it[7]) * p.head_chunks + hc) * p.hkv + kvh;
       float* const sl = p.part + (slot * 4 + wave) * (32 * D) + 4 * lane;
+      const float f = row_scale(1.f);
 #pragma unroll
       for (int db = 0; db < DB; ++db)
 #pragma unroll
         for (int g = 0; g < 4; ++g) {
           f32x4 v;
 #pragma unroll
-          for (int jj = 0; jj < 4; ++jj) v[jj] = dq[db][4 * g + jj];
+          for (int jj = 0; jj < 4; ++jj) v[jj] = BIAS ? f * dq[db][4 * g + jj] : dq[db][4 * g + jj];
           *reinterpret_cast<f32x4*>(sl + 256 * (4 * db + g)) = v;
         }
     }
@@ -272,73 +330,16 @@ __device__ __forceinline__ void dq_tile(const DqParams& p, int b, char* smem) {
 
   // dQ rows out through this wave's share of the (now free) K/V buffers,
   // 1 KiB per store instruction
+  const float rscale = row_scale(gscale);
   store_rows<D, RPW>(
       smem + size_t(wave) * (32 * D * 4), active,
       [&](int db, int g) {
         f32x4 v;
 #pragma unroll
-        for (int jj = 0; jj < 4; ++jj) v[jj] = p.scale * dq[db][4 * g + jj];
+        for (int jj = 0; jj < 4; ++jj) v[jj] = rscale * dq[db][4 * g + jj];
         return v;
       },
       q0 + wave * RPW, q1, p.hq, kvh * p.group + hc * HPW, p.dq, nullptr);
-}
-
-// dQ of a query tile whose key range was split: the parts' slots added in
-// slot order (key order), scaled and stored. A workgroup takes one wave's 32
-// rows, a quarter of the columns per wave and four slots in flight at once, so
-// that few tiles still spread over the chip: bound by the latency of its reads.
-template <int D, int HPW>
-__global__ __launch_bounds__(256) void dq_combine_kernel(DqParams p) {
-  constexpr int RPW = 32 / HPW, KW = D / 32;  // KW: 16-byte pieces per lane
-  __shared__ __attribute__((aligned(16))) float st[32 * D];
-  const int lane = threadIdx.x & 63;
-  const int qw = blockIdx.x & 3, b = blockIdx.x >> 2;  // the rows' wave, the tile
-  const int kvh = b % p.hkv, rest = b / p.hkv, hc = rest % p.head_chunks;
-  const int32_t* e = p.comb + 8 * (rest / p.head_chunks);
-  const int q0 = e[0], q1 = e[1], first = e[2], n = e[3];
-  if (q0 + qw * RPW >= q1) return;
-  auto read = [&](f32x4 (&x)[KW], int s) {
-    const size_t slot = (size_t(first + s) * p.head_chunks + hc) * p.hkv + kvh;
-    const float* const o = p.part + (slot * 4 + qw) * (32 * D) + 256 * KW * wave_id() + 4 * lane;
-#pragma unroll
-    for (int k = 0; k < KW; ++k) x[k] = *reinterpret_cast<const f32x4*>(o + 256 * k);
-  };
-  f32x4 acc[KW], x[4][KW];
-  auto add = [&](const f32x4 (&y)[KW]) {
-#pragma unroll
-    for (int k = 0; k < KW; ++k)
-#pragma unroll
-      for (int j = 0; j < 4; ++j) acc[k][j] += y[k][j];
-  };
-  read(acc, 0);
-  for (int s = 1; s < n; s += 4) {
-#pragma unroll
-    for (int u = 0; u < 4; ++u) read(x[u], min(s + u, n - 1));
-#pragma unroll
-    for (int u = 0; u < 4; ++u)
-      if (s + u < n) add(x[u]);
-  }
-  store_rows_shared<D, RPW>(
-      st,
-      [&](int k) {
-        f32x4 v;
-#pragma unroll
-        for (int j = 0; j < 4; ++j) v[j] = p.scale * acc[k][j];
-        return v;
-      },
-      q0 + qw * RPW, q1, p.hq, kvh * p.group + hc * HPW, p.dq, nullptr);
-}
-
-template <int D>
-static hipError_t launch_dq_combine_d(const DqParams& p, int hpw, hipStream_t s) {
-  const dim3 grid(unsigned(p.n_comb) * p.hkv * p.head_chunks * 4), block(256);
-  switch (hpw) {
-    case 1: hipLaunchKernelGGL((dq_combine_kernel<D, 1>), grid, block, 0, s, p); break;
-    case 2: hipLaunchKernelGGL((dq_combine_kernel<D, 2>), grid, block, 0, s, p); break;
-    case 4: hipLaunchKernelGGL((dq_combine_kernel<D, 4>), grid, block, 0, s, p); break;
-    default: return hipErrorInvalidValue;
-  }
-  return hipGetLastError();
 }
 
 }  // namespace fck

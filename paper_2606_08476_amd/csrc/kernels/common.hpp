@@ -218,6 +218,13 @@ __device__ __forceinline__ uint32_t opaque(uint32_t x) {
   return x;
 }
 
+// The lane's index, counted anew: no register holds it until here.
+__device__ __forceinline__ uint32_t fresh_lane() {
+  uint32_t x;
+  asm volatile("v_mbcnt_lo_u32_b32 %0, -1, 0\n\tv_mbcnt_hi_u32_b32 %0, -1, %0" : "=v"(x));
+  return x;
+}
+
 // Asynchronous HBM-to-LDS copies. Lane i's 16 (or 4) bytes at `gbase` +
 // `voff` land at LDS byte address `lds` + 16*i (4*i); `gbase` and `lds` are
 // wave-uniform. The instruction is issued from inline assembly so that the
@@ -282,19 +289,21 @@ __device__ __forceinline__ int wave_id() {
 // offsets. Rows whose index within their block is at or past `nvalid`
 // repeat row nvalid-1 of the same block (finite data for masked rows, no
 // read past the range).
-template <int D, int ROWS, int NT = 256, int RPB = ROWS>
+// FRESH, for kernels that have no register to spare across their loop: a ragged
+// tile's offsets (1), or every tile's (2), from the lane's index counted anew.
+template <int D, int ROWS, int NT = 256, int RPB = ROWS, int FRESH = 0>
 struct TileLoader {
   static constexpr int CH = D / 8;
   static constexpr int N = ROWS * CH / NT;
   static_assert((ROWS * CH) % NT == 0, "tile must be a multiple of NT chunks");
   static_assert(ROWS % RPB == 0, "whole blocks of rows");
-  uint32_t off[N];
+  uint32_t off[FRESH == 2 ? 1 : N];
   int row_stride, block_stride;
 
   __device__ __forceinline__ explicit TileLoader(int stride, int bstride = 0)
       : row_stride(stride), block_stride(bstride) {
 #pragma unroll
-    for (int u = 0; u < N; ++u) {
+    for (int u = 0; u < N && FRESH < 2; ++u) {
       const int L = u * NT + threadIdx.x;
       const int r = L / CH;
       off[u] = 2u * uint32_t((r % RPB) * stride + (r / RPB) * bstride + 8 * ((L % CH) ^ swz<D>(r)));
@@ -307,13 +316,23 @@ struct TileLoader {
   // the same with the tile's LDS byte address
   __device__ __forceinline__ void load_at(uint32_t tile, const u16* g, int nvalid) const {
     const uint32_t lds = tile + 1024u * wave_id();
-    if (nvalid >= RPB) {  // uniform: whole blocks, the offsets as computed
+    if constexpr (FRESH == 2) {
+      const int thread = 64 * wave_id() + int(fresh_lane());
+#pragma unroll
+      for (int u = 0; u < N; ++u) {
+        const int L = u * NT + thread, r = L / CH;
+        const uint32_t o = 2u * uint32_t(min(r % RPB, nvalid - 1) * row_stride + (r / RPB) * block_stride +
+                                         8 * ((L % CH) ^ swz<D>(r)));
+        lds_copy16(g, o, lds + 16u * NT * u);
+      }
+    } else if (nvalid >= RPB) {  // uniform: whole blocks, the offsets as computed
 #pragma unroll
       for (int u = 0; u < N; ++u) lds_copy16(g, off[u], lds + 16u * NT * u);
     } else {  // the last, ragged rows of a range: a per-lane select, no branch
+      const int thread = FRESH ? 64 * wave_id() + int(fresh_lane()) : int(threadIdx.x);
 #pragma unroll
       for (int u = 0; u < N; ++u) {
-        const int L = u * NT + threadIdx.x;
+        const int L = u * NT + thread;
         const int r = L / CH;
         const uint32_t alt = 2u * uint32_t((nvalid - 1) * row_stride + (r / RPB) * block_stride +
                                            8 * ((L % CH) ^ swz<D>(r)));

@@ -92,6 +92,13 @@ struct FwdParams {
   const int32_t* comb;
   int32_t n_comb;
   SlotGuard* guard[2];
+  // scored views (score.hpp): cap_in = 2 scale log2(e) / cap and cap2 = cap
+  // log2(e), 0 if not capped; slopes [hq] in log2 units, null if not biased; then
+  // the positions in their documents of local and received tokens
+  float cap_in, cap2;
+  const float* slopes;
+  const float* q_pos;
+  const float* recv_pos;
 };
 
 struct BwdParams {
@@ -117,6 +124,11 @@ struct BwdParams {
   float* dv_recv;
   int32_t t_q;
   float* dq;                // [t_q, hq, d] fp32, added into (atomic pass only)
+  // scored views, as in FwdParams
+  float cap_in, cap2;
+  const float* slopes;
+  const float* q_pos;
+  const float* recv_pos;
 };
 
 struct DqParams {
@@ -141,10 +153,20 @@ struct DqParams {
   float* part;
   const int32_t* comb;
   int32_t n_comb;
+  // scored views, as in FwdParams
+  float cap_in, cap2;
+  const float* slopes;
+  const float* q_pos;
+  const float* recv_pos;
 };
 
 hipError_t launch_fwd(const FwdParams& p, int d, int heads_per_tile, bool final_out,
                       hipStream_t s);
+// (the same for one kind of score, output and head dim, each in a source file of
+// its own, and the merge of a split view's chunks)
+template <int SC>
+hipError_t launch_fwd_sc(const FwdParams& p, int d, int heads_per_tile, int out, hipStream_t s);
+hipError_t launch_fwd_combine(const FwdParams& p, int d, int heads_per_tile, hipStream_t s);
 hipError_t launch_bwd_dq(const DqParams& p, int d, int heads_per_tile, hipStream_t s);
 hipError_t launch_bwd(const BwdParams& p, int d, hipStream_t s);
 // dK/dV with dQ added into p.dq by atomics (p.dq zeroed beforehand)
@@ -152,6 +174,13 @@ hipError_t launch_bwd_atomic(const BwdParams& p, int d, hipStream_t s);
 // dK/dV and dQ in one launch (dK/dV workgroups first)
 hipError_t launch_bwd_grid(const BwdParams& bp, const DqParams& dp, int d, int heads_per_tile,
                            hipStream_t s);
+// (the same for one kind of score each, and the sum of a split query tile's parts)
+template <int SC>
+hipError_t launch_bwd_grid_sc(const BwdParams& bp, const DqParams& dp, int d, int heads_per_tile,
+                              hipStream_t s);
+template <int SC>
+hipError_t launch_bwd_keys_sc(const BwdParams& p, int d, bool atomic_dq, hipStream_t s);
+hipError_t launch_dq_combine(const DqParams& p, int d, int heads_per_tile, hipStream_t s);
 hipError_t launch_bwd_reduce(const int32_t* entries, int32_t n, const float* part_k,
                              const float* part_v, int32_t hkv, int32_t d, float* dk_loc,
                              float* dv_loc, float* dk_recv, float* dv_recv, hipStream_t s);

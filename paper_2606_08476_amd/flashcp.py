@@ -27,14 +27,18 @@ ERRORS = {
 # every function the header declares
 EXPORTS = [
     "fc_plan_per_doc", "fc_plan_per_seq", "fc_plan_whole_lpt", "fc_plan_hybrid", "fc_plan_validate",
-    "fc_plan_stats", "fc_view_create", "fc_view_get_info", "fc_view_export", "fc_view_bind",
+    "fc_plan_stats", "fc_view_create", "fc_view_create_scored", "fc_view_get_score", "fc_view_get_info", "fc_view_export", "fc_view_bind",
     "fc_view_destroy", "fc_view_export_launch", "fc_view_export_split", "fc_workspace_size", "fc_kv_gather", "fc_attn_fwd",
     "fc_attn_fwd_partial", "fc_attn_fwd_partials", "fc_lse_merge", "fc_attn_bwd", "fc_bwd_preprocess",
     "fc_attn_bwd_pass", "fc_attn_bwd_dkdv", "fc_attn_bwd_dq", "fc_attn_bwd_noalloc", "fc_last_error",
+    "fc_rope_freqs", "fc_rope_fwd", "fc_kv_gather_rope", "fc_rope_bwd",
 ]
 
 # bytes of the static device scratch behind fc_attn_bwd_noalloc (flashcp.h)
 NOALLOC_SCRATCH_BYTES = 64 * 1024 * 1024
+
+# the caps and slopes a view takes (flashcp.h)
+CAP_MIN, CAP_MAX, SLOPE_MAX = 2.0 ** -6, 1024.0, 1024.0
 
 
 class FlashCPError(RuntimeError):
@@ -50,6 +54,20 @@ class Shard(C.Structure):
 class TileCfg(C.Structure):
     _fields_ = [("bm_fwd", C.c_int32), ("bn_fwd", C.c_int32), ("bm_bwd", C.c_int32),
                 ("bn_bwd", C.c_int32)]
+
+
+class Score(C.Structure):
+    _fields_ = [("cap", C.c_float), ("slopes", C.c_void_p)]
+
+
+class RopeCfg(C.Structure):
+    _fields_ = [("dim", C.c_int32), ("interleaved", C.c_int32), ("packed_pos", C.c_int32),
+                ("amplitude", C.c_float), ("inv_freq", C.c_void_p)]
+
+
+class Rows(C.Structure):
+    _fields_ = [("in_", C.c_void_p), ("in_stride", C.c_int64), ("out", C.c_void_p),
+                ("out_stride", C.c_int64)]
 
 
 class ViewInfo(C.Structure):
@@ -86,6 +104,10 @@ def _signatures():
                           C.POINTER(C.c_double)],
         "fc_view_create": [I32P, C.c_int32, C.POINTER(Shard), C.c_int64, C.c_int32, C.c_int32,
                            C.c_int32, C.c_int32, C.c_int32, C.POINTER(TileCfg), C.POINTER(P)],
+        "fc_view_create_scored": [I32P, C.c_int32, C.POINTER(Shard), C.c_int64, C.c_int32, C.c_int32,
+                                  C.c_int32, C.c_int32, C.c_int32, C.POINTER(TileCfg),
+                                  C.POINTER(Score), C.POINTER(P)],
+        "fc_view_get_score": [P, C.POINTER(C.c_float), I32P, C.POINTER(C.c_float)],
         "fc_view_get_info": [P, C.POINTER(ViewInfo)],
         "fc_view_export": [P] + [I32P] * 11,
         "fc_view_bind": [P, P, C.c_size_t, P],
@@ -105,6 +127,11 @@ def _signatures():
                              C.c_size_t, P],
         "fc_attn_bwd_dkdv": [P, P, P, P, P, P, P, P, P, C.c_float, P, P, P, P, P, C.c_size_t, P],
         "fc_attn_bwd_dq": [P, P, P, P, P, P, P, P, P, C.c_float, P, P],
+        "fc_rope_freqs": [C.c_int32, C.c_double, C.c_int32, C.c_double, C.c_double, C.c_double,
+                          C.c_double, C.POINTER(C.c_double), C.POINTER(C.c_float)],
+        "fc_rope_fwd": [P, P, P, P, P, P],
+        "fc_kv_gather_rope": [P, P, P, P, C.c_int64, P, P, P, P, P],
+        "fc_rope_bwd": [P, P, C.c_int32, P, P, P, P, P, P],
         "fc_attn_bwd_noalloc": [P, P, P, P, P, P, P, P, P, P, C.c_float, C.c_int32, P, P, P, P,
                                 P, P],
     }
@@ -241,14 +268,28 @@ class View:
     """An fc_view handle plus, once bound, the device buffer holding its
     tables. Destroyed with ``close()`` (or when garbage collected).
     ``tiles``: (bm_fwd, bn_fwd, bm_bwd, bn_bwd), 0 for a default; None for
-    all defaults."""
+    all defaults. ``cap``, ``slopes`` (hq values): the score function of every
+    forward and backward call made with the view (fc_score), scores capped by cap *
+    tanh(x / cap) and less slopes[h] * distance; 0 and None for none."""
 
-    def __init__(self, cu, plan, cp: int, rank: int, hq: int, hkv: int, d: int, tiles=None):
+    def __init__(self, cu, plan, cp: int, rank: int, hq: int, hkv: int, d: int, tiles=None,
+                 cap: float = 0.0, slopes=None):
         a, p, n = _cu(cu)
         s, sp, m = _shards(plan)
         h = P()
         t = C.byref(TileCfg(*[int(x) for x in tiles])) if tiles is not None else None
-        _check(_addr().fc_view_create(p, n, sp, m, cp, rank, hq, hkv, d, t, C.byref(h)))
+        if cap or slopes is not None:
+            f = None
+            if slopes is not None:
+                f = np.ascontiguousarray(slopes, dtype=np.float32)
+                if f.shape != (hq,):
+                    raise ValueError(f"slopes has shape {f.shape}, expected ({hq},)")
+                f = f if f.flags.aligned else f.copy()
+            score = Score(float(cap), None if f is None else f.ctypes.data)
+            _check(_addr().fc_view_create_scored(p, n, sp, m, cp, rank, hq, hkv, d, t, C.byref(score),
+                                                 C.byref(h)))
+        else:
+            _check(_addr().fc_view_create(p, n, sp, m, cp, rank, hq, hkv, d, t, C.byref(h)))
         self._h = h
         self.meta = None
         info = ViewInfo()
@@ -265,6 +306,15 @@ class View:
         if d is None:
             d = self._info_dict = self._info.as_dict()
         return d
+
+    @property
+    def score(self):
+        """(cap, slopes): the view's score function, 0 and None for none."""
+        cap, biased = C.c_float(0), C.c_int32(0)
+        f = np.zeros(self._info.hq, dtype=np.float32)
+        _check(lib().fc_view_get_score(self.handle, C.byref(cap), C.byref(biased),
+                                       f.ctypes.data_as(C.POINTER(C.c_float))))
+        return cap.value, (f if biased.value else None)
 
     @property
     def handle(self):
@@ -550,3 +600,118 @@ def fc_attn_bwd_dq(view: View, q, k_loc, v_loc, k_recv, v_recv, lse, delta, dout
         _ptr(v_recv, KR, BF, "v_recv"), _ptr(lse, L, F32, "lse"),
         _ptr(delta, L, F32, "delta"), _ptr(dout, Q, BF, "dout"), float(scale),
         _ptr(dq, Q, F32, "dq"), _stream()))
+
+
+# --------------------------------------------------------------- rotary rows
+
+ROPE_SCALINGS = ("none", "linear", "base", "bands", "yarn")
+
+
+def fc_rope_freqs(dim: int, base: float = 10000.0, scaling: str = "none", factor: float = 1.0,
+                  low: float | None = None, high: float | None = None, context: float = 0.0):
+    """(radians per position of each of dim/2 pairs, amplitude). ``scaling``: one of
+    ROPE_SCALINGS; ``low`` and ``high`` turns default to 1 and 4 (bands) or 32 (yarn)."""
+    if scaling not in ROPE_SCALINGS:
+        raise ValueError(f"scaling must be one of {ROPE_SCALINGS}, got {scaling!r}")
+    low = 1.0 if low is None else low
+    high = (32.0 if scaling == "yarn" else 4.0) if high is None else high
+    w, amp = np.zeros(max(1, int(dim) // 2)), C.c_float(0)
+    _check(lib().fc_rope_freqs(int(dim), float(base), ROPE_SCALINGS.index(scaling), float(factor),
+                               float(low), float(high), float(context),
+                               w.ctypes.data_as(C.POINTER(C.c_double)), C.byref(amp)))
+    return w, amp.value
+
+
+class Rope:
+    """Rotary positions (fc_rope): the first ``dim`` values of each head turned, halves
+    apart or (``interleaved``) neighbours paired, by the position in the document or
+    (``packed_pos``) in the packed sequence. Frequencies from ``base`` and ``scaling``
+    (fc_rope_freqs), or given: ``inv_freq`` (dim/2 radians per position) and
+    ``amplitude``."""
+
+    def __init__(self, dim: int, base: float = 10000.0, interleaved: bool = False,
+                 packed_pos: bool = False, scaling: str = "none", factor: float = 1.0, low=None,
+                 high=None, context: float = 0.0, inv_freq=None, amplitude=None):
+        if inv_freq is None:
+            self.inv_freq, amp = fc_rope_freqs(dim, base, scaling, factor, low, high, context)
+        else:
+            self.inv_freq, amp = np.array(inv_freq, dtype=np.float64), 1.0
+            if self.inv_freq.shape != (int(dim) // 2,):
+                raise ValueError(f"inv_freq has shape {self.inv_freq.shape}, expected ({int(dim) // 2},)")
+        self.inv_freq.setflags(write=False)
+        self.amplitude = float(amp if amplitude is None else amplitude)
+        self._c = RopeCfg(int(dim), int(bool(interleaved)), int(bool(packed_pos)), self.amplitude,
+                          self.inv_freq.ctypes.data)
+        self._p = C.addressof(self._c)
+
+
+def _row_ptr(t, shape, dtype, name):
+    """(address, row stride) of a [T, H, d] tensor whose rows may lie apart."""
+    if not isinstance(t, _Tensor) or not t.is_cuda:
+        raise TypeError(f"{name} must be a device tensor")
+    if t.dtype is not dtype:
+        raise TypeError(f"{name} must be {dtype}, got {t.dtype}")
+    if t.shape != shape:
+        raise ValueError(f"{name} has shape {tuple(t.shape)}, expected {tuple(shape)}")
+    n, h, d = shape
+    s = t.stride()
+    if n == 0:
+        return t.data_ptr(), 0
+    if s[2] != 1 or (s[1] != d and h > 1) or (n > 1 and s[0] < h * d):
+        raise ValueError(f"{name} must have whole rows: strides {s}")
+    return t.data_ptr(), s[0] if n > 1 else 0
+
+
+def _rows(src, dst, shape, dtype, out_dtype, name):
+    """fc_rows of a tensor and its output, both given or both None."""
+    if src is None and dst is None:
+        return None
+    if src is None or dst is None:
+        raise ValueError(f"{name} and its output must be given together")
+    return Rows(*_row_ptr(src, shape, dtype, name), *_row_ptr(dst, shape, out_dtype, name + "_out"))
+
+
+def _ref(r):
+    return None if r is None else C.addressof(r)
+
+
+def fc_rope_fwd(view: View, rope, q, k, v, q_out, k_out, v_out):
+    """Own rows, bf16: q and k rotated, v copied, out of (slices of) projection
+    buffers. A tensor and its output may both be None; ``rope`` None copies."""
+    if torch is None:
+        _load_torch()
+    a = [_rows(q, q_out, view._q, BF, BF, "q"), _rows(k, k_out, view._kv, BF, BF, "k"),
+         _rows(v, v_out, view._kv, BF, BF, "v")]
+    _check(lib().fc_rope_fwd(view.handle, None if rope is None else rope._p, *map(_ref, a), _stream()))
+
+
+def fc_kv_gather_rope(view: View, rope, k_packed, v_packed, k_loc, v_loc, k_recv, v_recv):
+    """fc_kv_gather with the keys rotated on the way."""
+    if torch is None:
+        _load_torch()
+    KV, KR = view._kv, view._kvr
+    T = k_packed.shape[0]
+    packed = (T, KV[1], KV[2])
+    _check(lib().fc_kv_gather_rope(
+        view.handle, None if rope is None else rope._p, _ptr(k_packed, packed, BF, "k_packed"),
+        _ptr(v_packed, packed, BF, "v_packed"), T, _ptr(k_loc, KV, BF, "k_loc"),
+        _ptr(v_loc, KV, BF, "v_loc"), _ptr(k_recv, KR, BF, "k_recv"), _ptr(v_recv, KR, BF, "v_recv"),
+        _stream()))
+
+
+def fc_rope_bwd(view: View, rope, dq, dk_loc, dv_loc, dk_recv, dv_recv, dq_out, dk_loc_out,
+                dv_loc_out, dk_recv_out, dv_recv_out):
+    """fp32 gradients: dq and dk rotated back, dv as it is, into outputs of one type,
+    bf16 or fp32, which may be slices of a fused buffer. A tensor and its output may
+    both be None; ``rope`` None rounds or copies."""
+    if torch is None:
+        _load_torch()
+    out = next((t for t in (dq_out, dk_loc_out, dv_loc_out, dk_recv_out, dv_recv_out) if t is not None), None)
+    dt = F32 if isinstance(out, _Tensor) and out.dtype is F32 else BF
+    Q, KV, KR = view._q, view._kv, view._kvr
+    a = [_rows(dq, dq_out, Q, F32, dt, "dq"), _rows(dk_loc, dk_loc_out, KV, F32, dt, "dk_loc"),
+         _rows(dv_loc, dv_loc_out, KV, F32, dt, "dv_loc"),
+         _rows(dk_recv, dk_recv_out, KR, F32, dt, "dk_recv"),
+         _rows(dv_recv, dv_recv_out, KR, F32, dt, "dv_recv")]
+    _check(lib().fc_rope_bwd(view.handle, None if rope is None else rope._p, int(dt is BF),
+                             *map(_ref, a), _stream()))
