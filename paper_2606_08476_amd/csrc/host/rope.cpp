@@ -3,6 +3,7 @@
 // on the host before the launch, which is asynchronous on the caller's stream.
 #include <hip/hip_runtime.h>
 
+#include <algorithm>
 #include <cmath>
 #include <cstdint>
 #include <initializer_list>
@@ -53,11 +54,13 @@ int check_rope(const fc_rope* r, int32_t d) {
   return FC_OK;
 }
 
-// Radians per position as turns modulo 1, 64-bit fixed point.
+// Radians per position as turns modulo 1, 64-bit fixed point (|w| is within
+// FC_ROPE_FREQ_MAX, checked before).
 uint64_t turns(double w) {
-  const long double t = static_cast<long double>(w) / 6.283185307179586476925286766559L;
-  const long double f = std::ldexp(t - std::floor(t), 64);
-  return f >= 18446744073709551616.0L ? 0 : static_cast<uint64_t>(f);
+  constexpr long double kPerTurn = 0.15915494309189533576888376337251436L;
+  const long double t = w * kPerTurn;
+  const long double f = t - static_cast<int>(t);  // of w's sign, exact
+  return static_cast<uint64_t>(static_cast<int64_t>(f * 9223372036854775808.0L)) << 1;
 }
 
 // Validates the sets (null rows: skipped) and launches them together.
@@ -110,17 +113,19 @@ int run(const View& v, const fc_rope* rope, std::initializer_list<Set> sets, boo
       if ((!in_place && in[i].touches(out[j])) || (i < j && out[i].touches(out[j])))
         return fail(FC_ERR_INVALID_ARG, "rows written overlap rows of another tensor");
     }
-  // rows per workgroup: four units of 16 values per thread, fewer where the whole
+  // rows per workgroup: four units per thread, fewer where the whole
   // call would leave most of the card without work
   auto blocks_of = [&](int64_t units) {
     total = 0;
     for (int i = 0; i < p.n_sets; ++i) {
       fck::RopeRows& k = p.set[i];
-      const int64_t hu = int64_t(k.heads) * (v.d / 16);
+      const int64_t hu = int64_t(k.heads) * fck::rope_units(v.d, in_f32);
       int32_t per = 1;
       while (per < fck::kRopeRows && 2 * per * hu <= units) per *= 2;
       k.per_block = per;
       k.blocks = (k.rows + per - 1) / per;
+      k.step_t = int32_t(256 / hu);
+      k.step_q = int32_t(256 % hu);
       total += k.blocks;
     }
     return total;

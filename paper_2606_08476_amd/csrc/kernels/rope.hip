@@ -12,47 +12,43 @@
 // Bound by HBM: every row is read and written once. A workgroup takes a few tokens
 // of one tensor and puts their sines and cosines in LDS once, for every head (one
 // per thread and four tokens or so; held per lane they would be computed once per
-// eight heads). A thread then takes 16 values of a head (eight pairs), in 16-byte
-// pieces; a piece and its partner are read before either is written, so rows may be
-// rotated in place.
+// eight heads). A thread then takes units of two 16-byte pieces of a head: a pair's
+// two halves, or pieces half a head apart, read before either is written, so that
+// rows may be rotated in place.
 #include "common.hpp"
 #include "rope.hpp"
 
 namespace fck {
 
-// 8 values from / to memory, as fp32
+// A piece of a row: 16 bytes of it, 8 bf16 or 4 fp32 values, as fp32.
 template <bool F32>
-__device__ __forceinline__ void load8(float (&x)[8], const void* p, int64_t e) {
-  if constexpr (F32) {
-    const f32x4* q = reinterpret_cast<const f32x4*>(static_cast<const float*>(p) + e);
-    const f32x4 a = q[0], b = q[1];
+struct Piece {
+  static constexpr int V = F32 ? 4 : 8;
+  typedef uint32_t word __attribute__((ext_vector_type(4)));
+  static __device__ __forceinline__ void load(float (&x)[V], const void* p, int64_t e) {
+    const word w = *reinterpret_cast<const word*>(static_cast<const char*>(p) + e * (16 / V));
 #pragma unroll
-    for (int j = 0; j < 4; ++j) {
-      x[j] = a[j];
-      x[4 + j] = b[j];
-    }
-  } else {
-    const uint4 w = *reinterpret_cast<const uint4*>(static_cast<const u16*>(p) + e);
-    const uint32_t v[4] = {w.x, w.y, w.z, w.w};
-#pragma unroll
-    for (int j = 0; j < 4; ++j) {
-      x[2 * j] = bf2f(u16(v[j] & 0xffff));
-      x[2 * j + 1] = bf2f(u16(v[j] >> 16));
-    }
+    for (int j = 0; j < V; ++j)
+      x[j] = __uint_as_float(F32 ? w[j] : j & 1 ? w[j / 2] & 0xffff0000u : w[j / 2] << 16);
   }
-}
-template <bool F32>
-__device__ __forceinline__ void store8(void* p, int64_t e, const float (&x)[8]) {
-  if constexpr (F32) {
-    f32x4* q = reinterpret_cast<f32x4*>(static_cast<float*>(p) + e);
-    q[0] = f32x4{x[0], x[1], x[2], x[3]};
-    q[1] = f32x4{x[4], x[5], x[6], x[7]};
-  } else {
-    uint32_t v[4];
+};
+// V values stored, 16 bytes of fp32 or V of bf16, not to be kept in the L2: another
+// kernel is the next to read them. Against plain stores: own rows of 32/8 heads of
+// 128 over 64K tokens and 8 ranks 43.5 -> 39.2 us, their gather 87.9 -> 82.2.
+template <bool F32, int V>
+__device__ __forceinline__ void store(void* p, int64_t e, const float (&x)[V]) {
+  constexpr int N = F32 ? V : V / 2;
+  typedef uint32_t word __attribute__((ext_vector_type(N)));
+  word w;
 #pragma unroll
-    for (int j = 0; j < 4; ++j) v[j] = uint32_t(f2bf(x[2 * j])) | uint32_t(f2bf(x[2 * j + 1])) << 16;
-    *reinterpret_cast<uint4*>(static_cast<u16*>(p) + e) = make_uint4(v[0], v[1], v[2], v[3]);
+  for (int j = 0; j < N; ++j) {
+    if constexpr (F32)
+      w[j] = __float_as_uint(x[j]);
+    else
+      w[j] = uint32_t(f2bf(x[2 * j])) | uint32_t(f2bf(x[2 * j + 1])) << 16;
   }
+  word* q = reinterpret_cast<word*>(static_cast<char*>(p) + e * (F32 ? 4 : 2));
+  __builtin_nontemporal_store(w, q);
 }
 
 // The unaligned layout (halves that are no multiple of 8 values apart): single values.
@@ -70,38 +66,38 @@ __device__ __forceinline__ void store1(void* p, int64_t e, float x) {
 
 template <int D, int LAYOUT, bool IN32, bool OUT32>
 __global__ __launch_bounds__(256) void rope_kernel(RopeParams p) {
-  constexpr int U = D / 16;  // units of 16 values per head
+  constexpr int V = Piece<IN32>::V, U = D / (2 * V);  // units of two pieces per head
   __shared__ __attribute__((aligned(16))) float cs[2][kRopeRows * D / 2];
   __shared__ int32_t pos[kRopeRows];
   // this workgroup's tensor and rows
-  int b = blockIdx.x;
+  int blk = blockIdx.x;
   RopeRows s = p.set[0];
 #pragma unroll
   for (int i = 1; i < kRopeSets; ++i)
-    if (i < p.n_sets && b >= s.blocks) {
-      b -= s.blocks;
+    if (i < p.n_sets && blk >= s.blocks) {
+      blk -= s.blocks;
       s = p.set[i];
     }
-  const int r0 = b * s.per_block, n = min(s.per_block, s.rows - r0);
+  const int r0 = blk * s.per_block, n = min(s.per_block, s.rows - r0);
   const int tid = threadIdx.x;
-  if (tid < n) {
-    const int r = r0 + tid;
-    int x = s.gpos[r];
-    if (!p.packed_pos) {
-      int i = s.first[r / 64];
-      while (r >= p.seg[4 * i + s.end]) ++i;
-      x -= p.seg[4 * i + 2];
-    }
-    pos[tid] = x;
-  }
-  __syncthreads();
   if (s.rotate) {
+    if (tid < n) {
+      const int r = r0 + tid;
+      int x = s.gpos[r];
+      if (!p.packed_pos) {
+        int i = s.first[r / 64];
+        while (r >= p.seg[4 * i + s.end]) ++i;
+        x -= p.seg[4 * i + 2];
+      }
+      pos[tid] = x;
+    }
+    __syncthreads();
     for (int i = tid; i < n * (D / 2); i += 256) {
       const int j = i % (D / 2);
       float c = 1.f, sn = 0.f;
       if (j < p.pairs) {
-        const uint64_t t = p.turn[j] * uint64_t(uint32_t(pos[i / (D / 2)]));
-        sincospif(float(int32_t(t >> 32)) * 0x1p-31f, &sn, &c);
+        const uint64_t turn = p.turn[j] * uint64_t(uint32_t(pos[i / (D / 2)]));
+        sincospif(float(int32_t(turn >> 32)) * 0x1p-31f, &sn, &c);
         c *= p.amplitude;
         sn *= p.amplitude * p.sign;
       }
@@ -110,55 +106,67 @@ __global__ __launch_bounds__(256) void rope_kernel(RopeParams p) {
     }
     __syncthreads();
   }
+
   const int hu = s.heads * U;  // units per row
   const int half = p.pairs;    // values between a pair's halves
+  // unit q of row t; 256 units further with each step
+  int t = tid / hu, q = tid % hu;
   for (int i = tid; i < n * hu; i += 256) {
-    const int t = i / hu, h = (i % hu) / U, u = i % U;
+    const int h = q / U, u = q % U;
     const int64_t src = s.gather ? s.gather[r0 + t] : r0 + t;
     const int64_t in = src * s.in_stride + h * D, out = int64_t(r0 + t) * s.out_stride + h * D;
-    const float* c = cs[0] + t * (D / 2) + 8 * u;
-    const float* sn = cs[1] + t * (D / 2) + 8 * u;
+    const float* c = cs[0] + t * (D / 2);
+    const float* sn = cs[1] + t * (D / 2);
+    t += s.step_t;
+    q += s.step_q;
+    if (q >= hu) {
+      q -= hu;
+      ++t;
+    }
     if (LAYOUT == kRopeHalvesOdd && s.rotate) {
-      for (int j = 0; j < 8; ++j) {
-        const int q = 8 * u + j;  // pair q, or values of the rest two by two
-        const int ea = q < half ? q : 2 * q, eb = q < half ? q + half : 2 * q + 1;
+      for (int j = V * u; j < V * (u + 1); ++j) {
+        // pair j, or values of the rest two by two
+        const int ea = j < half ? j : 2 * j, eb = j < half ? j + half : 2 * j + 1;
         const float xa = load1<IN32>(s.in, in + ea), xb = load1<IN32>(s.in, in + eb);
-        store1<OUT32>(s.out, out + ea, xa * c[j] - xb * sn[j]);
-        store1<OUT32>(s.out, out + eb, xb * c[j] + xa * sn[j]);
+        store1<OUT32>(s.out, out + ea, j < half ? xa * c[j] - xb * sn[j] : xa);
+        store1<OUT32>(s.out, out + eb, j < half ? xb * c[j] + xa * sn[j] : xb);
       }
       continue;
     }
-    // the unit's two pieces of 8 values: halves apart where it is rotated so,
-    // neighbours elsewhere
-    int ea = 16 * u, eb = ea + 8;
-    if (LAYOUT == kRopeHalves && s.rotate && 8 * u < half) {
-      ea = 8 * u;
-      eb = ea + half;
+    // the unit's two pieces: pairs' halves where they are rotated so, elsewhere
+    // pieces from either half of the values, so that the lanes' lie side by side
+    int ea = V * u, eb = ea + D / 2;
+    const bool pairs = LAYOUT == kRopeHalves && s.rotate && ea < half;
+    if (LAYOUT == kRopeHalves && s.rotate) {
+      ea += pairs ? 0 : half;
+      eb = pairs ? ea + half : ea + (D / 2 - half);
     }
-    float a[8], bb[8];
-    load8<IN32>(a, s.in, in + ea);
-    load8<IN32>(bb, s.in, in + eb);
-    if (s.rotate) {
-      if (LAYOUT == kRopeNeighbours) {
+    float a[V], b[V];
+    Piece<IN32>::load(a, s.in, in + ea);
+    Piece<IN32>::load(b, s.in, in + eb);
+    // (what is not rotated is not multiplied either: 0 times an infinity beside it)
+    if (LAYOUT == kRopeNeighbours && s.rotate) {
 #pragma unroll
-        for (int j = 0; j < 4; ++j) {
-          const float x0 = a[2 * j], x1 = a[2 * j + 1], y0 = bb[2 * j], y1 = bb[2 * j + 1];
-          a[2 * j] = x0 * c[j] - x1 * sn[j];
-          a[2 * j + 1] = x1 * c[j] + x0 * sn[j];
-          bb[2 * j] = y0 * c[4 + j] - y1 * sn[4 + j];
-          bb[2 * j + 1] = y1 * c[4 + j] + y0 * sn[4 + j];
-        }
-      } else {
-#pragma unroll
-        for (int j = 0; j < 8; ++j) {
-          const float x = a[j], y = bb[j];
-          a[j] = x * c[j] - y * sn[j];
-          bb[j] = y * c[j] + x * sn[j];
-        }
+      for (int j = 0; j < V / 2; ++j) {
+        auto turn = [&](float& x0, float& x1, int i) {
+          const float y0 = x0 * c[i] - x1 * sn[i], y1 = x1 * c[i] + x0 * sn[i];
+          x0 = i < half ? y0 : x0;
+          x1 = i < half ? y1 : x1;
+        };
+        turn(a[2 * j], a[2 * j + 1], ea / 2 + j);
+        turn(b[2 * j], b[2 * j + 1], eb / 2 + j);
       }
     }
-    store8<OUT32>(s.out, out + ea, a);
-    store8<OUT32>(s.out, out + eb, bb);
+    if (pairs) {
+#pragma unroll
+      for (int j = 0; j < V; ++j) {
+        const float x = a[j], y = b[j], cc = c[ea + j], ss = sn[ea + j];
+        a[j] = x * cc - y * ss;
+        b[j] = y * cc + x * ss;
+      }
+    }
+    store<OUT32>(s.out, out + ea, a);
+    store<OUT32>(s.out, out + eb, b);
   }
 }
 

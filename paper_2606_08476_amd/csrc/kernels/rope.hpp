@@ -20,10 +20,13 @@ struct RopeRows {
   int32_t rotate;         // 0: copied (or rounded) only
   int32_t per_block;      // rows per workgroup, a power of two up to kRopeRows
   int32_t blocks;
+  int32_t step_t, step_q;  // 256 units further: rows, and units of a row
 };
 
 constexpr int kRopeRows = 32;
 constexpr int kRopeSets = 5;
+// units of two 16-byte pieces of a row
+constexpr int rope_units(int d, bool in_f32) { return d / (in_f32 ? 8 : 16); }
 
 struct RopeParams {
   RopeRows set[kRopeSets];

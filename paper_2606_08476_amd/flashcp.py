@@ -11,6 +11,7 @@ from __future__ import annotations
 
 import ctypes as C
 import os
+import struct
 
 import numpy as np
 
@@ -63,11 +64,6 @@ class Score(C.Structure):
 class RopeCfg(C.Structure):
     _fields_ = [("dim", C.c_int32), ("interleaved", C.c_int32), ("packed_pos", C.c_int32),
                 ("amplitude", C.c_float), ("inv_freq", C.c_void_p)]
-
-
-class Rows(C.Structure):
-    _fields_ = [("in_", C.c_void_p), ("in_stride", C.c_int64), ("out", C.c_void_p),
-                ("out_stride", C.c_int64)]
 
 
 class ViewInfo(C.Structure):
@@ -647,32 +643,28 @@ class Rope:
 
 def _row_ptr(t, shape, dtype, name):
     """(address, row stride) of a [T, H, d] tensor whose rows may lie apart."""
-    if not isinstance(t, _Tensor) or not t.is_cuda:
-        raise TypeError(f"{name} must be a device tensor")
-    if t.dtype is not dtype:
-        raise TypeError(f"{name} must be {dtype}, got {t.dtype}")
-    if t.shape != shape:
-        raise ValueError(f"{name} has shape {tuple(t.shape)}, expected {tuple(shape)}")
-    n, h, d = shape
-    s = t.stride()
-    if n == 0:
-        return t.data_ptr(), 0
-    if s[2] != 1 or (s[1] != d and h > 1) or (n > 1 and s[0] < h * d):
-        raise ValueError(f"{name} must have whole rows: strides {s}")
-    return t.data_ptr(), s[0] if n > 1 else 0
+    if isinstance(t, _Tensor) and t.dtype is dtype and t.shape == shape and t.is_cuda:
+        s0, s1, s2 = t.stride()
+        n, h, d = shape
+        if n <= 1 and t.is_contiguous():
+            return t.data_ptr(), 0
+        if s2 == 1 and (s1 == d or h == 1) and s0 >= h * d:
+            return t.data_ptr(), s0
+        raise ValueError(f"{name} must have whole rows: strides {(s0, s1, s2)}")
+    _ptr(t, shape, dtype, name)  # says what is wrong
+    raise ValueError(f"{name} is not a row tensor")
 
 
 def _rows(src, dst, shape, dtype, out_dtype, name):
-    """fc_rows of a tensor and its output, both given or both None."""
+    """fc_rows of a tensor and its output (as bytes), both given or both None."""
     if src is None and dst is None:
         return None
     if src is None or dst is None:
         raise ValueError(f"{name} and its output must be given together")
-    return Rows(*_row_ptr(src, shape, dtype, name), *_row_ptr(dst, shape, out_dtype, name + "_out"))
+    return _ROWS.pack(*_row_ptr(src, shape, dtype, name), *_row_ptr(dst, shape, out_dtype, name))
 
 
-def _ref(r):
-    return None if r is None else C.addressof(r)
+_ROWS = struct.Struct("PqPq")
 
 
 def fc_rope_fwd(view: View, rope, q, k, v, q_out, k_out, v_out):
@@ -682,7 +674,7 @@ def fc_rope_fwd(view: View, rope, q, k, v, q_out, k_out, v_out):
         _load_torch()
     a = [_rows(q, q_out, view._q, BF, BF, "q"), _rows(k, k_out, view._kv, BF, BF, "k"),
          _rows(v, v_out, view._kv, BF, BF, "v")]
-    _check(lib().fc_rope_fwd(view.handle, None if rope is None else rope._p, *map(_ref, a), _stream()))
+    _check(lib().fc_rope_fwd(view.handle, None if rope is None else rope._p, *a, _stream()))
 
 
 def fc_kv_gather_rope(view: View, rope, k_packed, v_packed, k_loc, v_loc, k_recv, v_recv):
@@ -714,4 +706,4 @@ def fc_rope_bwd(view: View, rope, dq, dk_loc, dv_loc, dk_recv, dv_recv, dq_out, 
          _rows(dk_recv, dk_recv_out, KR, F32, dt, "dk_recv"),
          _rows(dv_recv, dv_recv_out, KR, F32, dt, "dv_recv")]
     _check(lib().fc_rope_bwd(view.handle, None if rope is None else rope._p, int(dt is BF),
-                             *map(_ref, a), _stream()))
+                             *a, _stream()))

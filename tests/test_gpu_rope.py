@@ -198,6 +198,15 @@ def test_edge_values(dev):  # noqa: F811
     bad = ~torch.isfinite(o)
     where = {tuple(i) for i in torch.nonzero(bad).tolist()}
     assert where and where <= {(3, 0, 5), (3, 0, 37), (7, 1, 8), (7, 1, 40)}
+    # beside them, values that are not rotated stay as they are
+    for m in (32, 24, 6):
+        for inter in (False, True):
+            x = r.randn(40, 2)
+            x[:, :, m::2] = float("inf")
+            o = r.nan(40, 2)
+            F.fc_rope_fwd(r.view, F.Rope(m, interleaved=inter), x, None, None, o, None, None)
+            torch.cuda.synchronize()
+            assert torch.equal(o[..., m:], x[..., m:]) and torch.isfinite(o[..., :m]).all()
 
 
 def test_refusals(dev):  # noqa: F811

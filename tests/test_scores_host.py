@@ -133,11 +133,7 @@ def test_frequency_refusals():
 
 
 def _rows(i=256, o=1 << 20, si=0, so=0):
-    return F.Rows(i, si, o, so)
-
-
-def _r(x):
-    return None if x is None else C.addressof(x)
+    return F._ROWS.pack(i, si, o, so)
 
 
 def test_rows_rejected_before_launch():
@@ -147,10 +143,10 @@ def test_rows_rejected_before_launch():
     v = _view()
     h, rope = v.handle, F.Rope(64)
     q, k, w = _rows(), _rows(1 << 22, 1 << 23), _rows(1 << 24, 1 << 25)
-    assert lib.fc_rope_fwd(h, rope._p, _r(q), _r(k), _r(w), None) == -5
-    assert lib.fc_rope_bwd(h, rope._p, 1, _r(q), _r(k), None, None, None, None) == -5
+    assert lib.fc_rope_fwd(h, rope._p, q, k, w, None) == -5
+    assert lib.fc_rope_bwd(h, rope._p, 1, q, k, None, None, None, None) == -5
     assert lib.fc_kv_gather_rope(h, rope._p, 256, 256, 1000, 256, 256, 256, 256, None) == -5
-    assert lib.fc_rope_fwd(None, rope._p, _r(q), _r(k), _r(w), None) == -1
+    assert lib.fc_rope_fwd(None, rope._p, q, k, w, None) == -1
     v.close()
 
 
