@@ -545,6 +545,9 @@ int build_view(const int32_t* cu, int32_t n_docs, const fc_shard* shards, int64_
         if (l > (int64_t(1) << 24))
           return fail(FC_ERR_UNSUPPORTED, "a document of a view with slopes has more than 2^24 tokens");
       v.slopes.assign(score->slopes, score->slopes + hq);
+      v.biased = true;
+    } else if (v.cap > fck::kCapFixed) {
+      v.slopes.assign(size_t(hq), 0.f);
     }
   }
   // tile shapes: the forward / dQ query tile is 128 / (heads per workgroup)
@@ -669,7 +672,7 @@ int fc_view_get_score(fc_view view, float* cap, int32_t* biased, float* slopes) 
   if (!view) return fail(FC_ERR_INVALID_ARG, "view is null");
   const View& v = *reinterpret_cast<View*>(view);
   if (cap) *cap = v.cap;
-  if (biased) *biased = !v.slopes.empty();
+  if (biased) *biased = v.biased;
   if (slopes)
     for (int32_t h = 0; h < v.hq; ++h) slopes[h] = v.slopes.empty() ? 0.f : v.slopes[h];
   return FC_OK;

@@ -14,8 +14,10 @@ struct View {
   int32_t hq = 0, hkv = 0, d = 0, heads_per_tile = 1;
   int32_t bm_fwd = 0, bn_fwd = 0, bm_bwd = 0, bn_bwd = 0;
 
-  // score function: cap (0: none) and slopes per query head (empty: none), as given
+  // score function: cap (0: none) and slopes per query head (empty: none), as given;
+  // a cap above kCapFixed without slopes has slopes of 0 here
   float cap = 0;
+  bool biased = false;
   std::vector<float> slopes;
 
   std::vector<int32_t> q_gpos, recv_gpos;   // global positions, local / receive order

@@ -84,6 +84,9 @@ struct FwdLds {
 template <int D, int HPW, int OUT, int SC>
 __device__ __forceinline__ void fwd_tile(const FwdParams& p, char* smem) {
   constexpr bool CAP = SC & kScoreCap, BIAS = SC & kScoreBias;
+  // capped scores alone lie within the cap: the reference of every row's exponentials
+  // is kCapTop below the cap, and neither maxima nor rescaling are needed
+  constexpr bool FIXED = SC == kScoreCap;
   constexpr bool FINAL = OUT == kOutFinal, MERGED = OUT == kOutMerged, UNIT = OUT == kOutUnit;
   constexpr bool CHUNKS = OUT == kOutChunks;
   constexpr bool PAIRED = OUT == kOutPaired || MERGED;
@@ -196,7 +199,7 @@ __device__ __forceinline__ void fwd_tile(const FwdParams& p, char* smem) {
   // LSE of a row with sum `tot`, natural log (BIAS: and what rounding left out of the
   // row's share, from values read again rather than held across the loop)
   auto row_lse = [&](float tot) {
-    float l = m + __log2f(tot);
+    float l = (FIXED ? cap2 - kCapTop : m) + __log2f(tot);
     if constexpr (BIAS) {
       const int ln = int(fresh_lane()) & 31, r = min(q0 + wave * RPW + ln % RPW, q1 - 1);
       float rest;
@@ -361,6 +364,7 @@ __device__ __forceinline__ void fwd_tile(const FwdParams& p, char* smem) {
   // scores of tile j: keys past the range and, on diagonal tiles, keys after
   // the query are masked (element i of block mb is key k0 + 4*half +
   // cst(mb, i), visible iff cst < rel: one compare per score, edge tiles only)
+  constexpr float kHidden = FIXED ? INFINITY : -INFINITY;  // no weight
   auto mask = [&](f32x16 (&s)[2], int j) {
     const bool rs = j < n_r;
     const int k0 = rs ? r0 + j * BN : l0 + (j - n_r) * BN;
@@ -374,13 +378,17 @@ __device__ __forceinline__ void fwd_tile(const FwdParams& p, char* smem) {
       for (int mb = 0; mb < 2; ++mb)
 #pragma unroll
         for (int i = 0; i < 16; ++i)
-          s[mb][i] = mb * 32 + 8 * (i >> 2) + (i & 3) < rel ? s[mb][i] : -INFINITY;
+          s[mb][i] = mb * 32 + 8 * (i >> 2) + (i & 3) < rel ? s[mb][i] : kHidden;
     }
   };
   // SC: element e of a tile's products as a score in log2 units; kp: positions
   // of the keys of its group of four
+  // (FIXED: up to r, which the exponential takes the rest of the way)
   auto score = [&](f32x16 (&s)[2], int e, const f32x4& kp) {
-    s[e / 16][e % 16] = score_of<SC>(s[e / 16][e % 16], c, cap2,
+    if constexpr (FIXED)
+      s[e / 16][e % 16] = cap_r(s[e / 16][e % 16], c);
+    else
+      s[e / 16][e % 16] = score_of<SC>(s[e / 16][e % 16], c, cap2,
                                      BIAS ? __builtin_fmaf(slope2, kp[e & 3], off2) : off2);
   };
   auto read_pos = [&](int e, uint32_t ofs) {  // of elements e & ~3 .. +3
@@ -411,7 +419,7 @@ __device__ __forceinline__ void fwd_tile(const FwdParams& p, char* smem) {
       }
     }
     mask(sa, 0);
-    mxa = row_max(sa);
+    if constexpr (!FIXED) mxa = row_max(sa);
   }
   // every wave has read K of tile 0 before iteration 0 copies tile 2 into
   // the same buffer
@@ -430,9 +438,10 @@ __device__ __forceinline__ void fwd_tile(const FwdParams& p, char* smem) {
   constexpr int NS = 2 * KS + 4 * DB;  // score slots, then PV slots
   constexpr int EX = 32 / (2 * KS);    // exponentials per score slot
   // SC: elements SS per slot become scores from PV slot 1 on, and the maxima follow
-  constexpr int SS = 64 / DB / 4;
-  constexpr int MX = SC ? 2 + 32 / SS : 3;  // first PV slot that takes maxima
-  constexpr int MPS = (32 + (4 * DB - MX) - 1) / (4 * DB - MX);  // maxima per slot
+  // (FIXED: in every PV slot, with no maxima to follow)
+  constexpr int SS = FIXED ? 8 / DB : 16 / DB, S0 = FIXED ? 0 : 1;
+  constexpr int MX = FIXED ? 4 * DB : SC ? 2 + 32 / SS : 3;  // first PV slot that takes maxima
+  constexpr int MPS = FIXED ? 0 : (32 + (4 * DB - MX) - 1) / (4 * DB - MX + FIXED);  // maxima per slot
   auto step = [&](int j, auto par, f32x16 (&sc)[2], float mxc, f32x16 (&sn)[2], float& mxn) {
     constexpr int PAR = decltype(par)::value;
     constexpr uint32_t KN = (1 - PAR) * TILE, VC = (2 + PAR) * TILE;
@@ -448,8 +457,8 @@ __device__ __forceinline__ void fwd_tile(const FwdParams& p, char* smem) {
     if (active) {
       // a row's output is rescaled only when its maximum grows by more than
       // the headroom; rows that do not grow keep their maximum and scale by 1
-      const bool grow = mxc > m + kLazy;  // implies mxc > m
-      if (__any(grow)) {
+      const bool grow = !FIXED && mxc > m + kLazy;  // implies mxc > m
+      if (!FIXED && __any(grow)) {
         const float alpha =
             !grow ? 1.f : m == -INFINITY ? 0.f : __builtin_amdgcn_exp2f(m - mxc);
         m = grow ? mxc : m;
@@ -481,7 +490,8 @@ __device__ __forceinline__ void fwd_tile(const FwdParams& p, char* smem) {
         }
       };
       float ps = 0.f, mx = -INFINITY;
-      f32x4 kp[SS / 4];  // BIAS: positions of the next slot's keys
+      constexpr int KP = SS < 4 ? 1 : SS / 4;
+      f32x4 kp[KP];  // BIAS: positions of the next slot's keys
       sn[0] = zero16();
       sn[1] = zero16();
       rd(0);
@@ -493,8 +503,10 @@ __device__ __forceinline__ void fwd_tile(const FwdParams& p, char* smem) {
           sn[n % 2] = mfma32(ring[n % 3], qreg[n / 2], sn[n % 2]);
 #pragma unroll
           for (int e = n * EX; e < (n + 1) * EX; ++e) {
-            const float x = __builtin_amdgcn_exp2f(SC ? sc[e / 16][e % 16] - mref
-                                                      : __builtin_fmaf(sc[e / 16][e % 16], c, -mref));
+            const float y = sc[e / 16][e % 16];
+            const float x = __builtin_amdgcn_exp2f(FIXED ? __builtin_fmaf(y, -2.f * cap2, kCapTop)
+                                                   : SC  ? y - mref
+                                                         : __builtin_fmaf(y, c, -mref));
             sc[e / 16][e % 16] = x;
             ps += x;
             if (e % 8 == 7) {
@@ -511,14 +523,14 @@ __device__ __forceinline__ void fwd_tile(const FwdParams& p, char* smem) {
         } else {
           constexpr int u = n - 2 * KS;
           oacc[u % DB] = mfma32(ring[n % 3], pb[u / DB], oacc[u % DB]);
-          if constexpr (SC && u <= 32 / SS) {
-            if constexpr (u >= 1) {
+          if constexpr (SC && u < S0 + 32 / SS) {
+            if constexpr (u >= S0) {
 #pragma unroll
-              for (int e = (u - 1) * SS; e < u * SS; ++e) score(sn, e, kp[e / 4 % (SS / 4)]);
+              for (int e = (u - S0) * SS; e < (u - S0 + 1) * SS; ++e) score(sn, e, kp[e / 4 % KP]);
             }
             if constexpr (BIAS && u < 32 / SS) {
 #pragma unroll
-              for (int i = 0; i < SS / 4; ++i) kp[i] = read_pos(u * SS + 4 * i, OP + (1 - PAR) * 256);
+              for (int i = 0; i < KP; ++i) kp[i] = read_pos(u * SS + 4 * i, OP + (1 - PAR) * 256);
             }
           }
           if constexpr (u == MX - 1) mask(sn, j + 1);
@@ -527,7 +539,7 @@ __device__ __forceinline__ void fwd_tile(const FwdParams& p, char* smem) {
             for (int e = (u - MX) * MPS; e < (u - MX + 1) * MPS && e < 32; ++e)
               mx = fmaxf(mx, sn[e / 16][e % 16]);
           }
-          if constexpr (u == 4 * DB - 1) mxn = SC ? max_halves(mx) : max_halves(mx) * c;
+          if constexpr (u == 4 * DB - 1 && !FIXED) mxn = SC ? max_halves(mx) : max_halves(mx) * c;
         }
         __builtin_amdgcn_sched_barrier(0);
       });

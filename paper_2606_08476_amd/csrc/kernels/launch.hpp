@@ -53,6 +53,14 @@ struct SlotGuard {
   pid_t pid_ = 0;                   // of the process that made the events
 };
 
+// Forward with capped scores alone: exponentials of score - (cap2 - kCapTop), without
+// a row maximum. They lie from 2^(kCapTop - 2 cap2) to 2^kCapTop: for caps up to
+// kCapFixed within 2^-100 .. 2^60, whose sums and products with values from 2^-26 to
+// 2^36 are normal numbers at any length. Views with larger caps are launched as
+// biased ones, with slopes of 0 (32/8 heads of 128, 64K tokens over 8 ranks: 463 us
+// with the fixed reference, 511 with a running maximum, 555 as biased ones).
+constexpr float kCapTop = 60.f, kCapFixed = 55.f;
+
 struct FwdParams {
   const uint16_t* q;        // [t_q, hq, d] bf16
   const uint16_t* k_recv;   // [t_r, hkv, d]

@@ -47,6 +47,8 @@ SHAPES = {
 KINDS = {
     "cap30": (30.0, False, 6.0),
     "cap2": (2.0, False, 3.0),
+    "cap55": (55.0, False, 30.0),
+    "cap56": (56.0, False, 30.0),
     "cap1024": (1024.0, False, 1.0),
     "bias": (0.0, True, 3.0),
     "cap30_bias": (30.0, True, 3.0),

@@ -37,7 +37,7 @@ def test_the_score_function_is_kept():
     v = _view(cap=30.0, slopes=s)
     cap, got = v.score
     assert cap == 30.0 and got.tolist() == s
-    assert _view(cap=30.0).score == (30.0, None)
+    assert _view(cap=30.0).score == (30.0, None) and _view(cap=1000.0).score == (1000.0, None)
     cap, got = _view(slopes=np.zeros(4)).score
     assert cap == 0.0 and got.tolist() == [0.0] * 4
     assert _view().score == (0.0, None) and _view(cap=0.0).score == (0.0, None)
