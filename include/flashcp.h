@@ -206,9 +206,16 @@ typedef struct {
  * and no slopes: fc_view_create). The view carries the function: its tables hold
  * the slopes and the positions a bias counts, and every forward and backward call
  * below applies it; lse is the log-sum-exp of the scores it gives, and dq, dk are
- * the gradients through it. Inputs are finite, as for every view. Accuracy is that
- * of the uncapped calls: a capped score is within cap * 2^-21 of its value, and
- * 1 - tanh^2 is rounded to fp16 before dK's dS is rounded to bf16. */
+ * the gradients through it. Inputs are finite, as for every view, and with a cap and
+ * no slopes values of v are below 2^36. Accuracy is that of the uncapped calls: a
+ * capped score is within cap * 2^-21 of its value, and 1 - tanh^2 is rounded to fp16
+ * before dK's dS is rounded to bf16.
+ * Under steep slopes most keys of a long document have no weight left. Where slopes
+ * and lengths promise it, fc_attn_fwd and the backward calls that take a workspace
+ * bound the scores by the rows' norms (a pass over q and k of its own; its results
+ * are the last bytes that fc_workspace_size asks for, and with less workspace every
+ * key is visited) and leave out keys whose weights add up to less than 2^-76 of a
+ * row's. */
 int fc_view_create_scored(const int32_t* cu_seqlens, int32_t n_docs, const fc_shard* shards,
                           int64_t n_shards, int32_t cp, int32_t rank, int32_t hq, int32_t hkv,
                           int32_t d, const fc_tile_cfg* tiles, const fc_score* score, fc_view* out);

@@ -55,7 +55,8 @@ size_t whole_fwd_ws(const View& v, int32_t mode) {
   if (mode != FC_TWO_PASS || v.t_recv() == 0) return 0;
   return align_up((v.fwd_fused.size() / 8) * v.slot_bytes());
 }
-// The same, or the chunks' partials of a split view, in either mode.
+// The same, or the chunks' partials of a split view, in either mode (where a view
+// prunes, its row norms come behind them).
 size_t fwd_ws(const View& v, int32_t mode) {
   return v.fwd_chunk ? align_up(v.fwd_split_bytes()) : whole_fwd_ws(v, mode);
 }
@@ -63,6 +64,12 @@ size_t fwd_ws(const View& v, int32_t mode) {
 // holds every chunk's partial.
 bool split_fwd(const View& v, int32_t mode, const void* ws, size_t ws_bytes) {
   return v.fwd_chunk && ws && ws_bytes >= fwd_ws(v, mode);
+}
+// The row norms' place in a workspace of `bytes`, `before` of them taken (256-byte
+// aligned); null if the view does not prune or the rest is too small.
+float* norms_at(const View& v, void* ws, size_t bytes, size_t before) {
+  if (!v.prune || !ws || bytes < before + v.norm_bytes()) return nullptr;
+  return reinterpret_cast<float*>(static_cast<char*>(ws) + before);
 }
 // the backward pass's workspace: partial dK/dV of split key tiles, then
 // partial dQ of split query tiles
@@ -108,6 +115,7 @@ fck::FwdParams fwd_params(const View& v, const int32_t* items, int64_t n,
   p.head_chunks = p.group / v.heads_per_tile;
   p.scale_log2 = resolve_scale(scale, v.d) * 1.4426950408889634f;
   p.t_q = v.t_q();
+  p.t_r = v.t_recv();
   set_score(p, v, scale);
   return p;
 }
@@ -173,6 +181,7 @@ fck::BwdParams bwd_params(const View& v, const void* q, const void* k_loc, const
   p.dk_recv = dk_recv;
   p.dv_recv = dv_recv;
   p.t_q = v.t_q();
+  p.t_r = v.t_recv();
   set_score(p, v, scale);
   return p;
 }
@@ -222,8 +231,12 @@ int run_pass(const View& v, const void* q, const void* k_loc, const void* v_loc,
              hipStream_t s) {
   fck::BwdParams p = bwd_params(v, q, k_loc, v_loc, k_recv, v_recv, lse, delta, dout, scale,
                                 dk_loc, dv_loc, dk_recv, dv_recv, ws, v.part_bytes());
+  p.norms = norms_at(v, ws, ws_bytes, pass_ws(v));
   if (deterministic) {
+    if (p.norms) p.head_order = v.dev_meta + v.off.head_order;
     fck::DqParams d = dq_params(v, q, k_loc, v_loc, k_recv, v_recv, lse, delta, dout, scale, dq);
+    d.norms = p.norms;
+    d.head_order = p.head_order;
     if (split_dq(v, ws, ws_bytes)) {
       d.items = v.dev_meta + v.off.dq_items;
       d.n_items = int32_t(v.dq_items.size() / 8);
@@ -252,9 +265,9 @@ int fc_workspace_size(fc_view view, int32_t mode, size_t* fwd_bytes, size_t* bwd
   if (!view) return fail(FC_ERR_INVALID_ARG, "view is null");
   if (mode != FC_TWO_PASS && mode != FC_FUSED) return fail(FC_ERR_INVALID_ARG, "bad mode");
   const View& v = *reinterpret_cast<View*>(view);
-  if (fwd_bytes) *fwd_bytes = fwd_ws(v, mode);
-  if (bwd_bytes) *bwd_bytes = bwd_ws(v);
-  if (dkdv_bytes) *dkdv_bytes = pass_ws(v);
+  if (fwd_bytes) *fwd_bytes = fwd_ws(v, mode) + v.norm_bytes();
+  if (bwd_bytes) *bwd_bytes = bwd_ws(v) + v.norm_bytes();
+  if (dkdv_bytes) *dkdv_bytes = pass_ws(v) + v.norm_bytes();
   return FC_OK;
 }
 
@@ -358,12 +371,17 @@ int fc_attn_fwd(fc_view view, const void* q, const void* k_loc, const void* v_lo
                                       " bytes, need " + std::to_string(need));
   hipStream_t s = reinterpret_cast<hipStream_t>(stream);
   const int32_t* m = v->dev_meta;
+  auto reach = [&](fck::FwdParams& p) {
+    p.norms = norms_at(*v, ws, ws_bytes, fwd_ws(*v, mode));
+    if (p.norms && v->far_first) p.head_order = m + v->off.head_order;
+  };
   if (split_fwd(*v, mode, ws, ws_bytes)) {
     fck::FwdParams p = fwd_params(*v, nullptr, 0, q, k_loc, v_loc, k_recv, v_recv, scale);
     set_chunks(p, *v, ws);
     p.o_bf16 = static_cast<uint16_t*>(o);
     p.o_f32 = o_f32;
     p.lse = lse;
+    reach(p);
     return hip_status(fck::launch_fwd(p, v->d, v->heads_per_tile, true, s), "attn_fwd launch");
   }
   if (mode == FC_FUSED || v->t_recv() == 0) {
@@ -378,6 +396,7 @@ int fc_attn_fwd(fc_view view, const void* q, const void* k_loc, const void* v_lo
     p.o_bf16 = static_cast<uint16_t*>(o);
     p.o_f32 = o_f32;
     p.lse = lse;
+    reach(p);
     return hip_status(fck::launch_fwd(p, v->d, v->heads_per_tile, true, s), "attn_fwd launch");
   }
   // both partial passes and their log-sum-exp merge in one launch: each
@@ -390,6 +409,7 @@ int fc_attn_fwd(fc_view view, const void* q, const void* k_loc, const void* v_lo
   p.o_bf16 = static_cast<uint16_t*>(o);
   p.o_f32 = o_f32;
   p.lse = lse;
+  reach(p);
   return hip_status(fck::launch_fwd(p, v->d, v->heads_per_tile, true, s), "attn_fwd launch");
 }
 
@@ -445,6 +465,7 @@ int fc_attn_bwd_dkdv(fc_view view, const void* q, const void* k_loc, const void*
                                       " bytes, need " + std::to_string(need));
   fck::BwdParams p = bwd_params(*v, q, k_loc, v_loc, k_recv, v_recv, lse, delta, dout, scale,
                                 dk_loc, dv_loc, dk_recv, dv_recv, ws, need);
+  p.norms = norms_at(*v, ws, ws_bytes, pass_ws(*v));
   hipStream_t s = reinterpret_cast<hipStream_t>(stream);
   if (int rc = hip_status(fck::launch_bwd(p, v->d, s), "attn_bwd dK/dV launch")) return rc;
   return launch_reduce(*v, p, s);

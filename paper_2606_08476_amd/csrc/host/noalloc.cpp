@@ -65,6 +65,7 @@ int fc_attn_bwd_noalloc(fc_view view, const void* q, const void* k_loc, const vo
     return fail(FC_ERR_WORKSPACE, "view is not bound to device metadata");
   size_t need = 0;
   if (int rc = fc_workspace_size(view, FC_TWO_PASS, nullptr, &need, nullptr)) return rc;
+  need -= reinterpret_cast<const fc::View*>(view)->norm_bytes();  // (done without, if need be)
   if (need > kScratchBytes)
     return fail(FC_ERR_WORKSPACE, "backward workspace of " + std::to_string(need) +
                                       " bytes exceeds the " + std::to_string(kScratchBytes) +

@@ -21,6 +21,7 @@
 #include <algorithm>
 #include <cmath>
 #include <cstring>
+#include <functional>
 #include <numeric>
 
 #include "internal.hpp"
@@ -114,6 +115,7 @@ void View::build_tiles() {
       push8(bwd, {k0, k1, q0, s1, first_tile_at_or_after(q0, s1, bm_bwd, qa), 1, s, 0});
     }
   }
+  decide_prune();
   // largest-first launch orders (the lists themselves stay in map order)
   auto fwd_cost = [&](const std::vector<int32_t>& items) {
     std::vector<int64_t> c(items.size() / 8);
@@ -145,6 +147,7 @@ void View::build_bwd_launch() {
   const size_t n = bwd.size() / 8;
   int64_t total = 0;
   for (size_t i = 0; i < n; ++i) total += ceil_div(bwd[8 * i + 3] - bwd[8 * i + 2], bm_bwd) * G;
+  if (prune) total = int64_t(kept * double(total));
   const int64_t cap = std::max<int64_t>(16, (total * hkv + kSlotsResident - 1) / kSlotsResident);
   bwd_launch.clear();
   bwd_reduce.clear();
@@ -231,7 +234,7 @@ void View::build_dq_split() {
   for (size_t i = 0; i < nk; ++i) {
     const int32_t* it = &bwd_launch[8 * i];
     const double t = wg + dk2 * ceil_div(it[3] - it[2], 32 / hpi) * (G / hpi);
-    dk_sum += t * hkv;
+    dk_sum += (wg + kept * (t - wg)) * hkv;
     dk_max = std::max(dk_max, t);
   }
   const double wgs = double(hkv) * head_chunks();  // workgroups per item
@@ -246,7 +249,7 @@ void View::build_dq_split() {
   }
   const double start = double(nk) * hkv >= kSlotsResident ? dk_sum / kSlotsResident : 0;
   auto grid_us = [&](double parts, double most) {
-    const double fair = (dk_sum + wgs * (double(total) * dq2 + parts * wg)) / kSlotsResident;
+    const double fair = (dk_sum + wgs * (kept * double(total) * dq2 + parts * wg)) / kSlotsResident;
     return std::max({fair, dk_max, start + most * dq1 + wg});
   };
   const double whole = grid_us(double(n), longest);
@@ -333,7 +336,7 @@ void View::build_fwd_split() {
   // a launch of more workgroups than fit ends, on average, some way into the
   // longest of the items it starts last
   auto launch_us = [&](double units, double most, int64_t sum) {
-    const double fair = wgs * (double(sum) * f2 + units * wg) / kSlotsResident;
+    const double fair = wgs * (kept * double(sum) * f2 + units * wg) / kSlotsResident;
     const double tail = units * wgs > kSlotsResident ? 0.3 * most * f1 : 0;
     return std::max(fair + tail, most * f1 + wg);
   };
@@ -400,6 +403,59 @@ void View::build_fwd_split() {
   }
   for (int32_t i : lpt_order(cost))
     fwd_units.insert(fwd_units.end(), &items[8 * size_t(i)], &items[8 * size_t(i)] + 8);
+}
+
+// Whether looking for keys out of reach pays: it reads every row once more, and
+// leaves out, of each KV head's keys, what lies beyond the reach of the least steep
+// head of the group. Estimated for products of unit normal rows (whose bound is
+// log2(e) sqrt(d)); worth it from a tenth of the pairs on. Then also in which order
+// the forward takes its heads: by which the last workgroup, started when all before
+// it have been dealt to the resident slots, ends sooner (heads one after the other
+// run 8% slower, see score.hpp).
+void View::decide_prune() {
+  prune = far_first = false;
+  kept = 1;
+  if (!biased || hq > fck::kNormHeads) return;
+  const double bound = 2 * 1.4427 * std::sqrt(double(d)) + 100;
+  std::vector<double> far(static_cast<size_t>(hkv));
+  for (int32_t g = 0; g < hkv; ++g) {
+    const float* s = &slopes[size_t(g) * (hq / hkv)];
+    far[size_t(g)] = bound / (1.4427 * double(*std::min_element(s, s + hq / hkv)));
+  }
+  std::sort(far.begin(), far.end(), std::greater<double>());
+  const size_t n = fwd_fused.size() / 8;
+  std::vector<int32_t> order(n);  // items, most keys first
+  std::iota(order.begin(), order.end(), 0);
+  auto keys = [&](int32_t i) {
+    const int32_t* it = &fwd_fused[8 * size_t(i)];
+    return double(it[3] - it[2]) + (it[5] - it[4]);
+  };
+  std::stable_sort(order.begin(), order.end(), [&](int32_t a, int32_t b) { return keys(a) > keys(b); });
+  // (keys by distance, evenly over the document up to the tile)
+  auto seen = [&](int32_t i, double r) {
+    return keys(i) * std::min(1.0, r / std::max(1.0, double(q_pos[size_t(fwd_fused[8 * size_t(i)])])));
+  };
+  double all = 0, some = 0, turn_end = 0, first_end = 0, dealt = 0;
+  for (int32_t i : order)
+    for (double r : far) {
+      const int32_t* it = &fwd_fused[8 * size_t(i)];
+      const double x = seen(i, r);
+      all += (it[1] - it[0]) * keys(i);
+      some += (it[1] - it[0]) * x;
+      turn_end = std::max(turn_end, dealt / kSlotsResident + x);
+      dealt += x * head_chunks();
+    }
+  prune = some < 0.9 * all;
+  if (!prune) return;
+  kept = some / all;
+  dealt = 0;
+  for (double r : far)
+    for (int32_t i : order) {
+      const double x = seen(i, r);
+      first_end = std::max(first_end, 1.08 * (dealt / kSlotsResident + x));
+      dealt += x * head_chunks();
+    }
+  far_first = first_end < turn_end;
 }
 
 // Every index the kernels will take from the tables, checked against the
@@ -510,6 +566,17 @@ void View::build_meta() {
     off.slopes = put_f(s2);
     off.q_pos = put_f(q_pos);
     off.recv_pos = put_f(recv_pos);
+    // by the least steep head of each group
+    const int32_t G = hq / hkv;
+    std::vector<float> least(static_cast<size_t>(hkv));
+    std::vector<int32_t> order(static_cast<size_t>(hkv));
+    for (int32_t j = 0; j < hkv; ++j) {
+      least[size_t(j)] = *std::min_element(&slopes[size_t(j) * G], &slopes[size_t(j) * G] + G);
+      order[size_t(j)] = j;
+    }
+    std::stable_sort(order.begin(), order.end(),
+                     [&](int32_t a, int32_t b) { return least[size_t(a)] < least[size_t(b)]; });
+    off.head_order = put(order);
   }
   if (meta.empty()) meta.resize(64, 0);
 }

@@ -19,6 +19,14 @@ struct View {
   float cap = 0;
   bool biased = false;
   std::vector<float> slopes;
+  // whether the final forward and the backward look for keys out of reach of a bias
+  // (they take norm_bytes of workspace more)
+  bool prune = false;
+  double kept = 1;         // share of the pairs then visited, estimated
+  bool far_first = false;  // the forward takes far reaching heads first, not in turn
+  size_t norm_bytes() const {
+    return prune ? size_t(hq + 2 * hkv) * fck::kNormParts * sizeof(float) : 0;
+  }
 
   std::vector<int32_t> q_gpos, recv_gpos;   // global positions, local / receive order
   std::vector<float> q_pos, recv_pos;       // with slopes: positions in the document
@@ -69,7 +77,8 @@ struct View {
     int64_t dq_items, dq_comb;
     int64_t fwd_units, fwd_comb;
     int64_t seg, first_q, first_r;
-    int64_t slopes, q_pos, recv_pos;        // with slopes only; fp32, slopes in log2 units
+    // with slopes only: fp32, slopes in log2 units; KV heads, least steep first
+    int64_t slopes, q_pos, recv_pos, head_order;
   } off{};
   const int32_t* dev_meta = nullptr;        // set by fc_view_bind
   // a split view's own slots, behind the tables in the bound buffer (null: the
@@ -84,6 +93,7 @@ struct View {
   void build_bwd_launch();
   void build_dq_split();
   void build_fwd_split();
+  void decide_prune();
   int32_t head_chunks() const { return hq / hkv / heads_per_tile; }
   // backward workspace: delta, the split key tiles' partial dK/dV, the split
   // query tiles' partial dQ

@@ -95,6 +95,10 @@ hipError_t launch_fwd_combine(const FwdParams& p, int d, int hpw, hipStream_t s)
 }
 
 template hipError_t launch_fwd_sc<0>(const FwdParams&, int, int, int, hipStream_t);
+// (in attn_fwd_cap.hip, attn_fwd_bias.hip and attn_fwd_cap_bias.hip)
+extern template hipError_t launch_fwd_sc<1>(const FwdParams&, int, int, int, hipStream_t);
+extern template hipError_t launch_fwd_sc<2>(const FwdParams&, int, int, int, hipStream_t);
+extern template hipError_t launch_fwd_sc<3>(const FwdParams&, int, int, int, hipStream_t);
 
 hipError_t launch_fwd(const FwdParams& p, int d, int heads_per_tile, bool final_out,
                       hipStream_t s) {
@@ -114,6 +118,10 @@ hipError_t launch_fwd(const FwdParams& p, int d, int heads_per_tile, bool final_
                   : p.o_f32_recv  ? (final_out ? kOutMerged : kOutPaired)
                   : final_out     ? kOutFinal
                                   : kOutPartial;
+  if (p.norms && final_out) {
+    const hipError_t e = launch_norms(p.norms, nullptr, p.k_loc, p.k_recv, p.t_q, p.t_r, p.hq, p.hkv, d, s);
+    if (e != hipSuccess) return e;
+  }
   switch (score_kind(p.cap2, p.slopes)) {
     case 0: return launch_fwd_sc<0>(p, d, heads_per_tile, out, s);
     case kScoreCap: return launch_fwd_sc<kScoreCap>(p, d, heads_per_tile, out, s);

@@ -98,10 +98,11 @@ __device__ __forceinline__ void dkdv_tile(const BwdParams& p, int b, char* smem)
   // the lane's index where it should not be held in a register up to here
   auto lane_here = [&]() { return SC ? fresh_lane() : opaque(uint32_t(lane)); };
   const int half = lane >> 5;
-  const int kvh = b % p.hkv;
-  const int item = b / p.hkv;  // the launch list is in launch order
+  int item;  // the launch list is in launch order
+  const int kvh = kv_head<BIAS>(p, b, p.n_items, item);
   const int32_t* it = p.items + 8 * item;  // launch list
-  const int k0 = it[0], k1 = it[1], q0 = it[2], q1 = it[3], qfull = it[4], src = it[5];
+  const int k0 = it[0], k1 = it[1], q0 = it[2], qfull = it[4], src = it[5];
+  int q1 = it[3];
   const u16* Kg = src ? p.k_recv : p.k_loc;
   const u16* Vg = src ? p.v_recv : p.v_loc;
   float* dKg = src ? p.dk_recv : p.dk_loc;
@@ -125,6 +126,20 @@ __device__ __forceinline__ void dkdv_tile(const BwdParams& p, int b, char* smem)
   // V rows of this lane's key as the B operand of dP = dO V^T
   bf16x8 vreg[KS];
 
+  if (BIAS && p.norms) {
+    // rows out of reach of the tile's last key, for every head of the group: none of
+    // the tile's keys has a weight in them
+    float qn = 0.f, s2 = INFINITY;
+    for (int i = 0; i < p.group; ++i) {
+      qn = fmaxf(qn, head_norm(p.norms, kvh * p.group + i));
+      s2 = fminf(s2, p.slopes[kvh * p.group + i]);
+    }
+    const float c = p.scale * kLog2e;
+    const float bl = score_bound<SC>(c, qn, head_norm(p.norms, p.hq + kvh), p.cap2);
+    const float bs = src ? score_bound<SC>(c, qn, head_norm(p.norms, p.hq + p.hkv + kvh), p.cap2) : bl;
+    const float far = (src ? p.recv_pos : p.q_pos)[k1 - 1] + reach(bs + bl, s2);
+    q1 = __builtin_amdgcn_readfirstlane(first_at(p.q_pos, q0, q1, nextafterf(far, INFINITY)));
+  }
   const int ntile = (q1 - q0 + RPI - 1) / RPI;
   const int n_it = ntile * (p.group / HPI);
 

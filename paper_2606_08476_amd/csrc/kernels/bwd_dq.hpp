@@ -51,11 +51,12 @@ __device__ __forceinline__ void dq_tile(const DqParams& p, int b, char* smem) {
 
   const int lane = threadIdx.x & 63, wave = wave_id();
   const int half = lane >> 5;
-  const int kvh = b % p.hkv;
-  const int rest = b / p.hkv;
+  int rest;
+  const int kvh = kv_head<BIAS>(p, b, p.n_items * p.head_chunks, rest);
   const int hc = rest % p.head_chunks;
   const int32_t* it = p.items + 8 * (rest / p.head_chunks);
-  const int q0 = it[0], q1 = it[1], r0 = it[2], r1 = it[3], l0 = it[4], l1 = it[5];
+  const int q0 = it[0], q1 = it[1], r1 = it[3], l1 = it[5];
+  int r0 = it[2], l0 = it[4];
   const int ldiag = it[6];
 
   // lane -> (query row, head) as in the forward: RPW rows of each of the
@@ -68,9 +69,12 @@ __device__ __forceinline__ void dq_tile(const DqParams& p, int b, char* smem) {
   const float sl2 = CAP ? p.cap_in : p.scale * kLog2e;
   const float gscale = CAP ? 4.f * p.scale : p.scale;
 
-  const int n_r = (r1 - r0 + BN - 1) / BN;
-  const int n_t = n_r + (l1 - l0 + BN - 1) / BN;
-
+  int n_r = 0, n_t = 0;
+  auto ranges = [&]() {
+    n_r = (r1 - r0 + BN - 1) / BN;
+    n_t = n_r + (l1 - l0 + BN - 1) / BN;
+  };
+  ranges();
   const TileLoader<D, BN, 256, BN, SC != 0> ld(p.hkv * D);
   auto fetch = [&](int j, uint32_t kofs) {
     const bool rs = j < n_r;
@@ -135,6 +139,24 @@ __device__ __forceinline__ void dq_tile(const DqParams& p, int b, char* smem) {
       qreg[ks] = lds_b128(smem, 2u * uint32_t(qb ^ (ks << 4)), 2 * TILE);
       oreg[ks] = lds_b128(smem, 2u * uint32_t(qb ^ (ks << 4)), 0);
     }
+  }
+  if (BIAS && p.norms) {
+    // the ranges start, whole tiles on, at the first key within reach of a row of the
+    // workgroup, given its LSE
+    float n2 = 0.f;
+#pragma unroll
+    for (int ks = 0; ks < KS; ++ks)
+#pragma unroll
+      for (int j = 0; j < 8; ++j)
+        n2 = __builtin_fmaf(active ? (float)qreg[ks][j] : 0.f, active ? (float)qreg[ks][j] : 0.f, n2);
+    n2 = sum_halves(n2);
+    const float qn = __builtin_sqrtf(n2 == n2 ? n2 : INFINITY), c = p.scale * kLog2e;
+    const float bl = score_bound<SC>(c, qn, head_norm(p.norms, p.hq + kvh), cap2);
+    const float br = score_bound<SC>(c, qn, head_norm(p.norms, p.hq + p.hkv + kvh), cap2);
+    const float at = p.q_pos[min(qrow, q1 - 1)];
+    skip_far<BN>(smem + OP, p.recv_pos, p.q_pos, qvalid ? at - reach(br - lse2, slope2) : INFINITY,
+                 qvalid ? at - reach(bl - lse2, slope2) : INFINITY, r0, r1, l0, l1);
+    ranges();
   }
   __syncthreads();  // every wave holds its rows before tile 0 overwrites them
   if (n_t > 0) fetch(0, 0);

@@ -162,11 +162,75 @@ __global__ __launch_bounds__(256) void bwd_reduce_kernel(const int32_t* __restri
   }
 }
 
+// Largest squared row norms per head (launch_norms): D / 8 lanes a row, four rows in
+// flight per lane, a maximum per head in LDS and one per head and block written out.
+template <int D>
+__global__ __launch_bounds__(1024) void norm_kernel(float* norms, const u16* q, const u16* kl,
+                                                    const u16* kr, int32_t t_q, int32_t t_r, int32_t hq,
+                                                    int32_t hkv) {
+  constexpr int LPR = D / 8, RPB = 1024 / LPR;  // lanes a row, rows at a time
+  constexpr int64_t STEP = int64_t(kNormParts) * RPB;
+  __shared__ uint32_t most[kNormHeads];
+  const int c = threadIdx.x % LPR;
+  auto tensor = [&](const u16* x, int t, int heads, float* out) {
+    for (int h = threadIdx.x; h < heads; h += 1024) most[h] = 0;
+    __syncthreads();
+    const int64_t rows = int64_t(t) * heads;
+    int64_t r = int64_t(blockIdx.x) * RPB + threadIdx.x / LPR;
+    int h = int(r % heads);
+    const int dh = int(STEP % heads);
+    for (; r < rows; r += 4 * STEP) {
+      uint4 w[4];
+#pragma unroll
+      for (int u = 0; u < 4; ++u)  // (past the last: the first again)
+        w[u] = reinterpret_cast<const uint4*>(x + (r + u * STEP < rows ? r + u * STEP : r) * D)[c];
+#pragma unroll
+      for (int u = 0; u < 4; ++u) {
+        const uint32_t v[4] = {w[u].x, w[u].y, w[u].z, w[u].w};
+        float n2 = 0.f;
+#pragma unroll
+        for (int j = 0; j < 4; ++j) {
+          const float a = bf2f(u16(v[j] & 0xffff)), b = bf2f(u16(v[j] >> 16));
+          n2 = __builtin_fmaf(a, a, n2);
+          n2 = __builtin_fmaf(b, b, n2);
+        }
+#pragma unroll
+        for (int s = LPR / 2; s >= 1; s >>= 1) n2 += __shfl_xor(n2, s);
+        // (not negative: ordered as their bits are)
+        if (c == 0 && r + u * STEP < rows)
+          atomicMax(&most[h], __float_as_uint(n2 == n2 ? n2 : INFINITY));
+        h += dh;
+        if (h >= heads) h -= heads;
+      }
+    }
+    __syncthreads();
+    for (int k = threadIdx.x; k < heads; k += 1024)
+      out[size_t(k) * kNormParts + blockIdx.x] = __uint_as_float(most[k]);
+    __syncthreads();
+  };
+  if (q) tensor(q, t_q, hq, norms);
+  tensor(kl, t_q, hkv, norms + size_t(hq) * kNormParts);
+  tensor(kr, t_r, hkv, norms + size_t(hq + hkv) * kNormParts);
+}
+
 // x[0 .. n) = 0 (n a multiple of 4; x 16-byte aligned)
 __global__ __launch_bounds__(256) void fill_zero_kernel(f32x4* x, int64_t n4) {
   const f32x4 z = {0.f, 0.f, 0.f, 0.f};
   for (int64_t i = int64_t(blockIdx.x) * 256 + threadIdx.x; i < n4; i += int64_t(gridDim.x) * 256)
     x[i] = z;
+}
+
+hipError_t launch_norms(float* norms, const uint16_t* q, const uint16_t* k_loc, const uint16_t* k_recv,
+                        int32_t t_q, int32_t t_r, int32_t hq, int32_t hkv, int d, hipStream_t s) {
+  if (hq > kNormHeads) return hipErrorInvalidValue;
+  const dim3 grid(kNormParts), block(1024);
+  if (d == 64)
+    hipLaunchKernelGGL(norm_kernel<64>, grid, block, 0, s, norms, q, k_loc, k_recv, t_q, t_r, hq, hkv);
+  else if (d == 128)
+    hipLaunchKernelGGL(norm_kernel<128>, grid, block, 0, s, norms, q, k_loc, k_recv, t_q, t_r, hq, hkv);
+  else
+    return hipErrorInvalidValue;
+  return hipGetLastError();
 }
 
 static unsigned grid_for(int64_t threads) {

@@ -112,11 +112,12 @@ __device__ __forceinline__ void fwd_tile(const FwdParams& p, char* smem) {
   const int lane = threadIdx.x & 63, wave = wave_id();
   const int half = lane >> 5;
   const int b = blockIdx.x;
-  const int kvh = b % p.hkv;
-  const int rest = b / p.hkv;
+  int rest;
+  const int kvh = kv_head<BIAS>(p, b, (UNIT ? p.n_units : p.n_items) * p.head_chunks, rest);
   const int hc = rest % p.head_chunks;
   const int32_t* it = (UNIT ? p.units : p.items) + 8 * (rest / p.head_chunks);
-  const int q0 = it[0], q1 = it[1], r0 = it[2], r1 = it[3], l0 = it[4], l1 = it[5];
+  const int q0 = it[0], q1 = it[1], r1 = it[3], l1 = it[5];
+  int r0 = it[2], l0 = it[4];
   const int ldiag = it[6];
   // a chunk of the source that this partial pass does not compute
   if (UNIT && !p.o_bf16 && !(r1 > r0 ? p.o_f32_recv : p.o_f32)) return;
@@ -138,6 +139,31 @@ __device__ __forceinline__ void fwd_tile(const FwdParams& p, char* smem) {
     float rest;
     slope2 = p.slopes[h];
     off2 = row_offset(off2, slope2, p.q_pos[min(qrow, q1 - 1)], rest);
+  }
+
+  bf16x8 qreg[KS];
+  auto read_q = [&]() {
+    const u16* qp = p.q + ((size_t)qrow * p.hq + h) * D + 8 * half;
+#pragma unroll
+    for (int ks = 0; ks < KS; ++ks)
+      qreg[ks] = qvalid ? *reinterpret_cast<const bf16x8*>(qp + 16 * ks) : zero8();
+  };
+  // BIAS, final output: the ranges start, whole tiles on, at the first key within
+  // reach of a row of the workgroup (the rows' norms from their registers)
+  if (BIAS && (FINAL || MERGED || (UNIT && p.o_bf16)) && p.norms) {
+    read_q();
+    float n2 = 0.f;
+#pragma unroll
+    for (int ks = 0; ks < KS; ++ks)
+#pragma unroll
+      for (int j = 0; j < 8; ++j) n2 = __builtin_fmaf((float)qreg[ks][j], (float)qreg[ks][j], n2);
+    n2 = sum_halves(n2);
+    const float qn = __builtin_sqrtf(n2 == n2 ? n2 : INFINITY);
+    const float bl = score_bound<SC>(p.scale_log2, qn, head_norm(p.norms, p.hq + kvh), cap2);
+    const float br = score_bound<SC>(p.scale_log2, qn, head_norm(p.norms, p.hq + p.hkv + kvh), cap2);
+    const float at = p.q_pos[min(qrow, q1 - 1)];
+    skip_far<BN>(smem + OP, p.recv_pos, p.q_pos, qvalid ? at - reach(br + bl, slope2) : INFINITY,
+                 qvalid ? at - reach(bl + bl, slope2) : INFINITY, r0, r1, l0, l1);
   }
 
   // key tiles: first the received range, then the local range
@@ -168,13 +194,7 @@ __device__ __forceinline__ void fwd_tile(const FwdParams& p, char* smem) {
   }
   if (n_t > 1) fetch(1, TILE, false);
 
-  bf16x8 qreg[KS];
-  {
-    const u16* qp = p.q + ((size_t)qrow * p.hq + h) * D + 8 * half;
-#pragma unroll
-    for (int ks = 0; ks < KS; ++ks)
-      qreg[ks] = qvalid ? *reinterpret_cast<const bf16x8*>(qp + 16 * ks) : zero8();
-  }
+  read_q();
 
   // per-lane LDS byte offsets of the MFMA operand reads (swizzled tiles):
   // K rows for k-step ks, and the two transpose reads of V^T block db

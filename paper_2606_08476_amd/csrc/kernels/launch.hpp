@@ -75,7 +75,7 @@ struct FwdParams {
   uint16_t* o_bf16;
   float* o_f32;
   float* lse;               // [hq, t_q]
-  int32_t t_q;
+  int32_t t_q, t_r;
   // both partials at once (non-null o_f32_recv): items carry a received and
   // a local range; the received partial goes to o_f32_recv/lse_recv, the
   // local one to o_f32/lse; with final output, the two are merged in the
@@ -107,6 +107,10 @@ struct FwdParams {
   const float* slopes;
   const float* q_pos;
   const float* recv_pos;
+  // null, or kNormParts floats per head; and then KV heads in launch order, null:
+  // in turn (score.hpp)
+  float* norms;
+  const int32_t* head_order;
 };
 
 struct BwdParams {
@@ -130,13 +134,17 @@ struct BwdParams {
   float* dv_loc;
   float* dk_recv;           // [t_r, hkv, d] fp32
   float* dv_recv;
-  int32_t t_q;
+  int32_t t_q, t_r;
   float* dq;                // [t_q, hq, d] fp32, added into (atomic pass only)
   // scored views, as in FwdParams
   float cap_in, cap2;
   const float* slopes;
   const float* q_pos;
   const float* recv_pos;
+  // null, or kNormParts floats per head; and then KV heads in launch order, null:
+  // in turn (score.hpp)
+  float* norms;
+  const int32_t* head_order;
 };
 
 struct DqParams {
@@ -166,7 +174,18 @@ struct DqParams {
   const float* slopes;
   const float* q_pos;
   const float* recv_pos;
+  // null, or kNormParts floats per head; and then KV heads in launch order, null:
+  // in turn (score.hpp)
+  float* norms;
+  const int32_t* head_order;
 };
+
+// blocks of the norm pass: partial maxima per head
+constexpr int kNormParts = 256, kNormHeads = 1024;
+// Largest squared norms of the rows of q (null: none) and of k_loc and k_recv, per
+// head and block: [hq | hkv | hkv][kNormParts].
+hipError_t launch_norms(float* norms, const uint16_t* q, const uint16_t* k_loc, const uint16_t* k_recv,
+                        int32_t t_q, int32_t t_r, int32_t hq, int32_t hkv, int d, hipStream_t s);
 
 hipError_t launch_fwd(const FwdParams& p, int d, int heads_per_tile, bool final_out,
                       hipStream_t s);

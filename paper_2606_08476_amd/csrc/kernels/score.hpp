@@ -21,6 +21,7 @@
 // left, which all scores of the row have in common. It drops out of the softmax,
 // and row_offset() gives what the row's LSE has to be corrected by.
 #include "common.hpp"
+#include "launch.hpp"
 
 namespace fck {
 
@@ -53,6 +54,115 @@ __device__ __forceinline__ float score_of(float x, float c, float cap2, float of
     return __builtin_fmaf(cap_r(x, c), -2.f * cap2, off);
   else
     return __builtin_fmaf(x, c, off);
+}
+
+// Keys out of reach. With |x| <= B = scale log2(e) |q| |k| (and <= cap2) for every key
+// of a source, and the row's own key among the local ones, a key at distance t has a
+// weight of at most 2^(B + B_local - slope2 t): where that is under 2^-kReach, all
+// such keys together (2^24 at most) are 2^-76 of the row's sum, 2^52 times less than
+// its last bit, and are not visited. Norms are the largest of a head's rows, in
+// kNormParts partial maxima of squares that launch_norms leaves (a NaN counts as
+// infinite, so that nothing is out of reach of it).
+constexpr float kReach = 100.f;
+
+__device__ __forceinline__ float wave_max(float x) {
+#pragma unroll
+  for (int w = 32; w >= 1; w >>= 1) x = fmaxf(x, __shfl_xor(x, w));
+  return x;
+}
+
+// Largest norm of a head's rows, for the wave.
+__device__ __forceinline__ float head_norm(const float* norms, int head) {
+  const f32x4 v = reinterpret_cast<const f32x4*>(norms + size_t(head) * kNormParts)[threadIdx.x & 63];
+  return __builtin_sqrtf(wave_max(fmaxf(fmaxf(v[0], v[1]), fmaxf(v[2], v[3]))));
+}
+
+// The bound B of a score's size, given the norms of q and k and scale log2(e).
+template <int SC>
+__device__ __forceinline__ float score_bound(float c, float qn, float kn, float cap2) {
+  const float b = fabsf(c) * qn * kn * 1.001f;  // (the norms' own roundings)
+  return (SC & kScoreCap) ? fminf(b, cap2) : b;
+}
+
+// KV head of workgroup b, and its index among those of the head; `per` of them.
+// Consecutive workgroups are on consecutive XCDs, so with eight KV heads each L2 serves
+// one of them. Where reach makes heads unequal, the heads are dealt to the XCDs in
+// turn, or (head_order) taken one after the other, the farthest reaching first, so
+// that no long workgroup starts late. One after the other, a head's rows lie 2 KB
+// apart and fewer of the memory's channels work at a time. Measured, an L2 per head /
+// in turn / farthest first: one 98K-token document, 32/8 heads of 128, slopes 2^-1/4
+// to 2^-8, forward 4101 / 2456 / 1360 us; 64K tokens of mixed documents, 8 ranks, two
+// passes 456 / 393 / 392, backward 1275 / 987 / 967, dK/dV alone 786 / 616 / 654;
+// 16/8 heads of 64, 32K tokens, cap and bias, forward 196 / 190 / 222.
+template <bool BIAS, class P>
+__device__ __forceinline__ int kv_head(const P& p, int b, int per, int& rest) {
+  if (BIAS && p.norms) {
+    if (p.head_order) {
+      rest = __builtin_amdgcn_readfirstlane(b % per);
+      return __builtin_amdgcn_readfirstlane(p.head_order[b / per]);
+    }
+    rest = b / p.hkv;
+    return __builtin_amdgcn_readfirstlane((b % p.hkv + rest) % p.hkv);
+  }
+  rest = b / p.hkv;
+  return b % p.hkv;
+}
+
+// How far a row's keys reach (b: what is known of the exponent without the bias).
+__device__ __forceinline__ float reach(float b, float slope2) {
+  const float r = (b + kReach) / slope2;
+  return r >= 0.f ? r : slope2 > 0.f && r < 0.f ? 0.f : INFINITY;
+}
+
+// First index of lo .. hi-1 whose position (ascending) is at least `cut`, hi if none;
+// by the whole wave, 64 probes at a time.
+__device__ __forceinline__ int first_at(const float* pos, int lo, int hi, float cut) {
+  const int lane = threadIdx.x & 63;
+  while (hi > lo) {
+    const int step = (hi - lo + 63) / 64, i = lo + lane * step;
+    const int n = __popcll(__ballot(i < hi && pos[min(i, hi - 1)] < cut));
+    if (step == 1 || n == 0) return lo + n;
+    hi = min(hi, lo + n * step);
+    lo += (n - 1) * step + 1;
+  }
+  return lo;
+}
+
+// The starts of a workgroup's received and local key ranges (r0 .. r1-1, l0 .. l1-1) moved
+// up, by whole tiles of BN keys, to the first key within reach of any of its rows: cr
+// and cl are this lane's positions under which a source's keys are out of reach
+// (infinite for a lane without a row). `lds`: 10 words that are free. Contains barriers;
+// two waves search, one range each, where there is anything to leave out.
+template <int BN>
+__device__ __forceinline__ void skip_far(char* lds, const float* recv_pos, const float* q_pos, float cr,
+                                         float cl, int& r0, int r1, int& l0, int l1) {
+  float* const cuts = reinterpret_cast<float*>(lds);
+  const int wave = wave_id();
+  cr = -wave_max(-cr);
+  cl = -wave_max(-cl);
+  if ((threadIdx.x & 63) == 0) {
+    cuts[2 * wave] = cr;
+    cuts[2 * wave + 1] = cl;
+  }
+  __syncthreads();
+  float mr = cuts[0], ml = cuts[1];
+#pragma unroll
+  for (int w = 1; w < 4; ++w) {
+    mr = fminf(mr, cuts[2 * w]);
+    ml = fminf(ml, cuts[2 * w + 1]);
+  }
+  if (mr > 0.f || ml > 0.f) {  // (no position is below 0)
+    int* const at = reinterpret_cast<int*>(lds) + 8;
+    if (wave < 2) {
+      const int a = wave ? l0 : r0, b = wave ? l1 : r1;
+      const int i = first_at(wave ? q_pos : recv_pos, a, b, wave ? ml : mr);
+      at[wave] = i >= b ? b : a + (i - a) / BN * BN;
+    }
+    __syncthreads();
+    r0 = __builtin_amdgcn_readfirstlane(at[0]);
+    l0 = __builtin_amdgcn_readfirstlane(at[1]);
+  }
+  __syncthreads();  // before the words are used again
 }
 
 }  // namespace fck

@@ -52,9 +52,13 @@ KINDS = {
     "cap1024": (1024.0, False, 1.0),
     "bias": (0.0, True, 3.0),
     "cap30_bias": (30.0, True, 3.0),
+    # every head steep: most keys of longer documents are out of reach, and skipped
+    "steep": (0.0, "steep", 1.0),
+    "cap30_steep": (30.0, "steep", 1.0),
 }
+LONG = [s for s in SHAPES if s.startswith(("split", "mixed"))]
 CASES = [(s, k) for s in SHAPES for k in KINDS if k in ("cap30", "bias", "cap30_bias") or s in
-         ("short_g4", "mixed_g1_d64", "split_g4")]
+         ("short_g4", "mixed_g1_d64", "split_g4") or ("steep" in k and s in LONG)]
 
 
 def slopes_of(hq):
@@ -74,7 +78,10 @@ class Run:
         kw.setdefault("plan", "per_doc")
         self.case = c = _cases.make_case(shape, "llama8b", seed=3, **kw)
         self.cap, biased, q_std = KINDS[kind]
-        self.slopes = slopes_of(c.hq) if biased else None
+        self.slopes = None
+        if biased:
+            # steep: a quarter to 2 per token
+            self.slopes = slopes_of(c.hq) if biased is True else np.linspace(0.25, 2.0, c.hq).astype(np.float32)
         x = {n: t.to(dev) for n, t in _cases.inputs(c).items()}
         self.q, self.do = x["q"] * q_std, x["do"]
         self.kv = [x[n].contiguous() for n in ("k_loc", "v_loc", "k_recv", "v_recv")]
@@ -136,6 +143,9 @@ def test_scored_views(shape, kind, dev):  # noqa: F811
     split = v.export_split()
     if shape.startswith("split"):
         assert split["fwd_chunk"] and len(split["dq_comb"])
+    if "steep" in kind and max(SHAPES[shape]["lens"]) > 700:
+        plain = F.View(c.cu, c.plan, c.cp, c.rank, c.hq, c.hkv, c.d, tiles=c.tiles)
+        assert v.workspace_size()[0] > plain.workspace_size()[0]   # row norms
     want, bnd = r.oracle(dout=r.do)
 
     # the forward, two passes and one
@@ -197,7 +207,17 @@ def test_scored_views(shape, kind, dev):  # noqa: F811
     assert all(torch.equal(a, b) for a, b in zip(step, det))
     assert all(torch.equal(a, b) for a, b in zip(alone[1:], det[1:]))
     far = lambda a, b: float((a - b).abs().max()) <= ORDER_TOL * max(1.0, float(b.abs().max()))  # noqa: E731
-    assert torch.equal(alone[0], det[0]) if not len(split["dq_comb"]) else far(alone[0], det[0])
+    # (steep: dQ alone has no row norms, and visits every key)
+    same = not len(split["dq_comb"]) and "steep" not in kind
+    assert torch.equal(alone[0], det[0]) if same else far(alone[0], det[0])
+
+    # without room for row norms, every key is visited: the same to rounding
+    if "steep" in kind:
+        wo = torch.empty(max(v.workspace_size()[2] - 1024, 1), dtype=torch.uint8, device=dev)
+        whole = r.grads()
+        F.fc_attn_bwd_pass(v, r.q, *r.kv, lse, delta, r.do, 0.0, *whole, wo)
+        torch.cuda.synchronize()
+        assert all(far(a, b) for a, b in zip(whole, det) if a.numel())
 
     # without allocation, and with dQ by atomics
     if v.workspace_size()[1] <= F.NOALLOC_SCRATCH_BYTES:
