@@ -150,7 +150,8 @@ __device__ __forceinline__ void fwd_tile(const FwdParams& p, char* smem) {
   };
   // BIAS, final output: the ranges start, whole tiles on, at the first key within
   // reach of a row of the workgroup (the rows' norms from their registers)
-  if (BIAS && (FINAL || MERGED || (UNIT && p.o_bf16)) && p.norms) {
+  const bool cut = BIAS && (FINAL || MERGED || (UNIT && p.o_bf16)) && p.norms;
+  if (cut) {
     read_q();
     float n2 = 0.f;
 #pragma unroll
@@ -174,9 +175,21 @@ __device__ __forceinline__ void fwd_tile(const FwdParams& p, char* smem) {
   // offset `ofs`; rows past the range repeat the last row (finite data;
   // those keys are masked)
   const TileLoader<D, BN, 256, BN, SC != 0> ld(p.hkv * D);
+  // first key of the j-th tile taken (BIAS: each source from its last tile on, or each
+  // of its chunks, the nearest keys first, so that maxima seldom grow)
+  auto tile_at = [&](int j) {
+    const bool rs = j < n_r;
+    int t = rs ? j : j - n_r;
+    if constexpr (BIAS) {
+      const int n = rs ? n_r : n_t - n_r;
+      const int c0 = CHUNKS ? t & -p.chunk : 0;  // (a power of 2)
+      t = c0 + (CHUNKS ? min(p.chunk, n - c0) : n) - 1 - (t - c0);
+    }
+    return (rs ? r0 : l0) + t * BN;
+  };
   auto fetch = [&](int j, uint32_t ofs, bool v) {
     const bool rs = j < n_r;
-    const int k0 = rs ? r0 + j * BN : l0 + (j - n_r) * BN;
+    const int k0 = tile_at(j);
     const int hi = rs ? r1 : l1;
     const size_t base = (size_t(k0) * p.hkv + kvh) * D;
     const u16* src = v ? (rs ? p.v_recv : p.v_loc) : (rs ? p.k_recv : p.k_loc);
@@ -194,7 +207,7 @@ __device__ __forceinline__ void fwd_tile(const FwdParams& p, char* smem) {
   }
   if (n_t > 1) fetch(1, TILE, false);
 
-  read_q();
+  if (!cut) read_q();
 
   // per-lane LDS byte offsets of the MFMA operand reads (swizzled tiles):
   // K rows for k-step ks, and the two transpose reads of V^T block db
@@ -387,7 +400,7 @@ __device__ __forceinline__ void fwd_tile(const FwdParams& p, char* smem) {
   constexpr float kHidden = FIXED ? INFINITY : -INFINITY;  // no weight
   auto mask = [&](f32x16 (&s)[2], int j) {
     const bool rs = j < n_r;
-    const int k0 = rs ? r0 + j * BN : l0 + (j - n_r) * BN;
+    const int k0 = tile_at(j);
     const int hi = rs ? r1 : l1;
     const bool diag = !rs && k0 >= ldiag;
     if (diag || k0 + BN > hi) {
