@@ -63,7 +63,7 @@ enum {
   FC_ERR_WORKSPACE = -5,   /* workspace too small, or view not bound */
   FC_ERR_HIP = -6,         /* a HIP runtime call failed */
   FC_ERR_CAPACITY = -7,    /* output array too small; *n_out holds the need */
-  FC_ERR_INTERNAL = -8     /* a table the library built failed its own bounds
+  FC_ERR_INTERNAL = -8     /* out of host memory, or a table the library built failed its own bounds
                               check before upload (a library bug) */
 };
 

@@ -81,7 +81,7 @@ int run(const View& v, const fc_rope* rope, std::initializer_list<Set> sets, boo
     if (!r.in || !r.out) return fail(FC_ERR_INVALID_ARG, "null tensor pointer");
     if (reinterpret_cast<uintptr_t>(r.in) % 16 || reinterpret_cast<uintptr_t>(r.out) % 16)
       return fail(FC_ERR_INVALID_ARG, "tensor pointers must be 16-byte aligned");
-    const int64_t w = int64_t(s.heads) * v.d, most = int64_t(1) << 32;
+    const int64_t w = int64_t(s.heads) * v.d, most = int64_t(1) << 28;
     const int64_t is = r.in_stride ? r.in_stride : w, os = r.out_stride ? r.out_stride : w;
     if (is < w || os < w || is > most || os > most || is * isz % 16 || os * osz % 16)
       return fail(FC_ERR_INVALID_ARG, "row strides must hold a row and be a multiple of 16 bytes");

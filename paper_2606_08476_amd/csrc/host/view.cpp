@@ -22,6 +22,8 @@
 #include <cmath>
 #include <cstring>
 #include <functional>
+#include <memory>
+#include <new>
 #include <numeric>
 
 #include "internal.hpp"
@@ -718,13 +720,15 @@ int fc_view_create_scored(const int32_t* cu, int32_t n_docs, const fc_shard* sha
   clear_error();
   if (!out) return fail(FC_ERR_INVALID_ARG, "out is null");
   *out = nullptr;
-  View* v = new View();
-  if (int rc = build_view(cu, n_docs, shards, n_shards, cp, rank, hq, hkv, d, tiles, score, *v)) {
-    delete v;
-    return rc;
+  try {
+    std::unique_ptr<View> v(new View());
+    if (int rc = build_view(cu, n_docs, shards, n_shards, cp, rank, hq, hkv, d, tiles, score, *v))
+      return rc;
+    *out = reinterpret_cast<fc_view>(v.release());
+    return FC_OK;
+  } catch (const std::bad_alloc&) {
+    return fail(FC_ERR_INTERNAL, "out of host memory");
   }
-  *out = reinterpret_cast<fc_view>(v);
-  return FC_OK;
 }
 
 int fc_view_create(const int32_t* cu, int32_t n_docs, const fc_shard* shards, int64_t n_shards,

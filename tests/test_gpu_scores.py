@@ -366,3 +366,57 @@ def test_every_rank_together_is_the_whole(dev):  # noqa: F811
             assert bool(((o - O[g]).abs() <= 2 * b["o32"][g]).all())
             assert bool(((l - L[:, g]).abs() <= 2 * b["lse"][:, g]).all())
     assert bool((seen == 3).all())
+
+
+@pytest.mark.parametrize("lens,cp,rank,hq,hkv,d,cap", [
+    # one long document, heads of very different reach: the far reaching ones first
+    ([60000], 8, 7, 32, 32, 64, 0.0), ([60000], 8, 7, 32, 8, 128, 30.0),
+    # documents of all lengths: heads in turn
+    ([9000, 40, 3000, 700, 1, 5000, 2000, 260], 2, 1, 32, 8, 128, 0.0),
+    ([9000, 40, 3000, 700, 1, 5000, 2000, 260], 2, 0, 6, 6, 64, 30.0),
+])
+def test_out_of_reach(lens, cp, rank, hq, hkv, d, cap, dev):  # noqa: F811
+    """Calls with room for row norms, which leave out keys out of reach, against the
+    same without (every key): what is left out is 2^-76 of a row, so the results are
+    the same but for the order of sums."""
+    c = _cases.make_case("reach", "llama8b", lens=lens, cp=cp, rank=rank, hq=hq, hkv=hkv, d=d, plan="per_doc")
+    slopes = (2.0 ** (-8.0 * np.arange(1, hq + 1) / hq)).astype(np.float32)
+    v = F.View(c.cu, c.plan, cp, rank, hq, hkv, d, cap=cap, slopes=slopes).bind(dev)
+    norms = 256 * 4 * (hq + 2 * hkv)
+    plain = F.View(c.cu, c.plan, cp, rank, hq, hkv, d)
+    assert v.workspace_size(F.FC_FUSED)[0] >= norms + (0 if plain.export_split()["fwd_chunk"] else
+                                                       plain.workspace_size(F.FC_FUSED)[0])
+    tq, tr = v.info["t_q"], v.info["t_recv"]
+    g = torch.Generator(device=dev).manual_seed(7)
+    e = lambda n, h: torch.randn(n, h, d, generator=g, device=dev, dtype=BF)  # noqa: E731
+    q, do = e(tq, hq), e(tq, hq)
+    # (queries of several sizes, one of which reaches far beyond the others)
+    q *= torch.tensor([0.25, 1.0, 3.0], device=dev)[torch.arange(tq, device=dev) % 3][:, None, None].to(BF)
+    q[tq // 2] *= 20
+    kv = e(tq, hkv), e(tq, hkv), e(tr, hkv), e(tr, hkv)
+    z = lambda *s, dt=F32: torch.full(s, float("nan"), device=dev, dtype=dt)  # noqa: E731
+
+    def run(short):
+        out = []
+        for mode in (F.FC_TWO_PASS, F.FC_FUSED):
+            o, o32, lse = z(tq, hq, d, dt=BF), z(tq, hq, d), z(hq, tq)
+            n = v.workspace_size(mode)[0] - (256 if short else 0)
+            F.fc_attn_fwd(v, q, *kv, 0.0, mode, o, o32, lse, torch.empty(n, dtype=torch.uint8, device=dev))
+            out += [o32, lse]
+        delta = z(hq, tq)
+        F.fc_bwd_preprocess(v, None, do, delta, o_f32=out[0])
+        n = v.workspace_size()[2] - (256 if short else 0)
+        ws = torch.empty(n, dtype=torch.uint8, device=dev)
+        for det in (True, False):
+            gr = [z(tq, hq, d), z(tq, hkv, d), z(tq, hkv, d), z(tr, hkv, d), z(tr, hkv, d)]
+            F.fc_attn_bwd_pass(v, q, *kv, out[1], delta, do, 0.0, *gr, ws, deterministic=det)
+            out += gr
+        torch.cuda.synchronize()
+        return out
+
+    for i, (a, b) in enumerate(zip(run(False), run(True))):
+        assert torch.isfinite(a).all() and torch.isfinite(b).all()
+        far = float((a - b).abs().max()) if a.numel() else 0.0
+        say(f"[gpu]   output {i}: {far:.1e} of {float(b.abs().max()) if b.numel() else 0:.1e}")
+        assert far <= ORDER_TOL * max(1.0, float(b.abs().max()) if b.numel() else 0.0), i
+    v.close()
