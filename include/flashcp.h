@@ -63,8 +63,9 @@ enum {
   FC_ERR_WORKSPACE = -5,   /* workspace too small, or view not bound */
   FC_ERR_HIP = -6,         /* a HIP runtime call failed */
   FC_ERR_CAPACITY = -7,    /* output array too small; *n_out holds the need */
-  FC_ERR_INTERNAL = -8     /* out of host memory, or a table the library built failed its own bounds
-                              check before upload (a library bug) */
+  FC_ERR_INTERNAL = -8     /* out of host memory; or a table the library built
+                              failed its own bounds check before upload (a
+                              library bug) */
 };
 
 /* fwd pass modes */
@@ -296,9 +297,10 @@ void fc_view_destroy(fc_view view);
 /* Workspace bytes fc_attn_fwd (for `mode`), fc_attn_bwd and, alone,
  * fc_attn_bwd_dkdv / fc_attn_bwd_pass take (any pointer may be NULL). On a view
  * whose long key ranges are split (fc_view_export_split) that includes the
- * query tiles' partial results. With a workspace too small for those the calls
- * below run the query tiles' ranges unsplit, and the results then differ in
- * their last bits; they are refused (FC_ERR_WORKSPACE) only with less than that
+ * query tiles' partial results, and on one that leaves out keys out of a bias's
+ * reach (fc_view_create_scored) the rows' norms. With a workspace too small for
+ * those the calls below run the query tiles' ranges unsplit, or visit every key,
+ * and the results then differ in their last bits; they are refused (FC_ERR_WORKSPACE) only with less than that
  * takes:
  *   fc_attn_fwd                          FC_TWO_PASS on a view that receives keys:
  *                                        the received partial O (128 rows x d
@@ -355,8 +357,8 @@ int fc_rope_freqs(int32_t dim, double base, int32_t scaling, double factor, doub
                   double context, double* inv_freq, float* amplitude);
 
 /* A tensor's rows on their way: token r's heads * d values from in + r * in_stride
- * to out + r * out_stride (strides in elements, a multiple of 16 bytes; 0: rows
- * without gaps, heads * d), so either may be a slice of a fused projection buffer.
+ * to out + r * out_stride (strides in elements, a multiple of 16 bytes, at most
+ * 2^28; 0: rows without gaps, heads * d), so either may be a slice of a fused projection buffer.
  * In place: the same address, stride and type. Otherwise no output may overlap an
  * input or another output (FC_ERR_INVALID_ARG). */
 typedef struct {

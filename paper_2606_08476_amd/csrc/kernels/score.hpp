@@ -81,7 +81,7 @@ __device__ __forceinline__ float head_norm(const float* norms, int head) {
 template <int SC>
 __device__ __forceinline__ float score_bound(float c, float qn, float kn, float cap2) {
   const float b = fabsf(c) * qn * kn * 1.001f;  // (the norms' own roundings)
-  return (SC & kScoreCap) ? fminf(b, cap2) : b;
+  return (SC & kScoreCap) && b < INFINITY ? fminf(b, cap2) : b;
 }
 
 // KV head of workgroup b, and its index among those of the head; `per` of them.

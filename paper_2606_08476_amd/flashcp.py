@@ -641,9 +641,21 @@ class Rope:
         self._p = C.addressof(self._c)
 
 
-def _row_ptr(t, shape, dtype, name):
+def _row_device(view):
+    """The device of a call on rows: the current one, which has to be the view's."""
+    if torch is None:
+        _load_torch()
+    dev = torch.cuda.current_device() if view.meta is not None else -1
+    if view.meta is not None and view.meta.get_device() != dev:
+        raise ValueError(f"the view is bound on device {view.meta.get_device()}, the current one is {dev}")
+    return dev
+
+
+def _row_ptr(t, shape, dtype, name, dev):
     """(address, row stride) of a [T, H, d] tensor whose rows may lie apart."""
     if isinstance(t, _Tensor) and t.dtype is dtype and t.shape == shape and t.is_cuda:
+        if dev >= 0 and t.get_device() != dev:
+            raise ValueError(f"{name} is on device {t.get_device()}, the current one is {dev}")
         s0, s1, s2 = t.stride()
         n, h, d = shape
         if n <= 1 and t.is_contiguous():
@@ -655,13 +667,14 @@ def _row_ptr(t, shape, dtype, name):
     raise ValueError(f"{name} is not a row tensor")
 
 
-def _rows(src, dst, shape, dtype, out_dtype, name):
+def _rows(src, dst, shape, dtype, out_dtype, name, dev):
     """fc_rows of a tensor and its output (as bytes), both given or both None."""
     if src is None and dst is None:
         return None
     if src is None or dst is None:
         raise ValueError(f"{name} and its output must be given together")
-    return _ROWS.pack(*_row_ptr(src, shape, dtype, name), *_row_ptr(dst, shape, out_dtype, name))
+    return _ROWS.pack(*_row_ptr(src, shape, dtype, name, dev),
+                      *_row_ptr(dst, shape, out_dtype, name + "'s output", dev))
 
 
 _ROWS = struct.Struct("PqPq")
@@ -670,17 +683,18 @@ _ROWS = struct.Struct("PqPq")
 def fc_rope_fwd(view: View, rope, q, k, v, q_out, k_out, v_out):
     """Own rows, bf16: q and k rotated, v copied, out of (slices of) projection
     buffers. A tensor and its output may both be None; ``rope`` None copies."""
-    if torch is None:
-        _load_torch()
-    a = [_rows(q, q_out, view._q, BF, BF, "q"), _rows(k, k_out, view._kv, BF, BF, "k"),
-         _rows(v, v_out, view._kv, BF, BF, "v")]
+    dev = _row_device(view)
+    a = [_rows(q, q_out, view._q, BF, BF, "q", dev), _rows(k, k_out, view._kv, BF, BF, "k", dev),
+         _rows(v, v_out, view._kv, BF, BF, "v", dev)]
     _check(lib().fc_rope_fwd(view.handle, None if rope is None else rope._p, *a, _stream()))
 
 
 def fc_kv_gather_rope(view: View, rope, k_packed, v_packed, k_loc, v_loc, k_recv, v_recv):
     """fc_kv_gather with the keys rotated on the way."""
-    if torch is None:
-        _load_torch()
+    dev = _row_device(view)
+    for t in (k_packed, v_packed, k_loc, v_loc, k_recv, v_recv):
+        if dev >= 0 and isinstance(t, _Tensor) and t.is_cuda and t.get_device() != dev:
+            raise ValueError(f"a tensor is on device {t.get_device()}, the current one is {dev}")
     KV, KR = view._kv, view._kvr
     T = k_packed.shape[0]
     packed = (T, KV[1], KV[2])
@@ -696,14 +710,13 @@ def fc_rope_bwd(view: View, rope, dq, dk_loc, dv_loc, dk_recv, dv_recv, dq_out, 
     """fp32 gradients: dq and dk rotated back, dv as it is, into outputs of one type,
     bf16 or fp32, which may be slices of a fused buffer. A tensor and its output may
     both be None; ``rope`` None rounds or copies."""
-    if torch is None:
-        _load_torch()
+    dev = _row_device(view)
     out = next((t for t in (dq_out, dk_loc_out, dv_loc_out, dk_recv_out, dv_recv_out) if t is not None), None)
     dt = F32 if isinstance(out, _Tensor) and out.dtype is F32 else BF
     Q, KV, KR = view._q, view._kv, view._kvr
-    a = [_rows(dq, dq_out, Q, F32, dt, "dq"), _rows(dk_loc, dk_loc_out, KV, F32, dt, "dk_loc"),
-         _rows(dv_loc, dv_loc_out, KV, F32, dt, "dv_loc"),
-         _rows(dk_recv, dk_recv_out, KR, F32, dt, "dk_recv"),
-         _rows(dv_recv, dv_recv_out, KR, F32, dt, "dv_recv")]
+    a = [_rows(dq, dq_out, Q, F32, dt, "dq", dev), _rows(dk_loc, dk_loc_out, KV, F32, dt, "dk_loc", dev),
+         _rows(dv_loc, dv_loc_out, KV, F32, dt, "dv_loc", dev),
+         _rows(dk_recv, dk_recv_out, KR, F32, dt, "dk_recv", dev),
+         _rows(dv_recv, dv_recv_out, KR, F32, dt, "dv_recv", dev)]
     _check(lib().fc_rope_bwd(view.handle, None if rope is None else rope._p, int(dt is BF),
                              *a, _stream()))

@@ -335,3 +335,21 @@ def test_a_training_step(kind, dev):  # noqa: F811
         near(n, got, x, e + 2.0 ** -8 * (x.abs() + e) + 2.0 ** -19 * x.abs().amax(-1, keepdim=True))
     for n, got, cut in (("dv", f[:, hq + hkv:], slice(0, tq)), ("dv_recv", rec[1], slice(tq, None))):
         near(n, got, want["dv"][cut], b["dv"][cut] + 2.0 ** -8 * (want["dv"][cut].abs() + b["dv"][cut]))
+
+
+def test_another_device(dev):  # noqa: F811
+    """Calls with a view, or tensors, of another device than the current one are refused."""
+    class Elsewhere:
+        def get_device(self):
+            return dev_index + 1
+    dev_index = torch.cuda.current_device()
+    r = Rank(dev)
+    q = r.randn(r.sizes[0], r.hq)
+    meta, r.view.meta = r.view.meta, Elsewhere()
+    none = [None] * 8
+    for call in (lambda: F.fc_rope_fwd(r.view, None, q, None, None, q, None, None),
+                 lambda: F.fc_kv_gather_rope(r.view, None, q, q, None, None, None, None),
+                 lambda: F.fc_rope_bwd(r.view, None, q, *none[:4], q, *none[:4])):
+        with pytest.raises(ValueError, match="device"):
+            call()
+    r.view.meta = meta

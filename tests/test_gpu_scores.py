@@ -420,3 +420,29 @@ def test_out_of_reach(lens, cp, rank, hq, hkv, d, cap, dev):  # noqa: F811
         say(f"[gpu]   output {i}: {far:.1e} of {float(b.abs().max()) if b.numel() else 0:.1e}")
         assert far <= ORDER_TOL * max(1.0, float(b.abs().max()) if b.numel() else 0.0), i
     v.close()
+
+
+def test_nothing_is_out_of_reach_of_a_nan(dev):  # noqa: F811
+    """A key that is not a number makes every row that sees it not one, near or far,
+    as it does where every key is visited."""
+    cu, cp, rank, hq, hkv, d = np.array([0, 9000, 12000], dtype=np.int32), 1, 0, 8, 2, 64
+    c = _cases.make_case("nan", "llama8b", lens=[9000, 3000], cp=cp, rank=rank, hq=hq, hkv=hkv, d=d, plan="per_doc")
+    slopes = np.full(hq, 0.5, dtype=np.float32)
+    v = F.View(c.cu, c.plan, cp, rank, hq, hkv, d, cap=30.0, slopes=slopes).bind(dev)
+    tq = v.info["t_q"]
+    assert v.workspace_size(F.FC_FUSED)[0] >= 256 * 4 * (hq + 2 * hkv)
+    g = torch.Generator(device=dev).manual_seed(7)
+    q, k, w = (torch.randn(tq, h, d, generator=g, device=dev, dtype=BF) for h in (hq, hkv, hkv))
+    k[20, 1] = float("nan")
+    none = torch.empty(0, hkv, d, dtype=BF, device=dev)
+    o, o32 = torch.zeros(tq, hq, d, dtype=BF, device=dev), torch.zeros(tq, hq, d, device=dev)
+    lse = torch.zeros(hq, tq, device=dev)
+    ws = torch.empty(v.workspace_size(F.FC_FUSED)[0], dtype=torch.uint8, device=dev)
+    F.fc_attn_fwd(v, q, k, w, none, none, 0.0, F.FC_FUSED, o, o32, lse, ws)
+    torch.cuda.synchronize()
+    want = torch.zeros(tq, hq, dtype=torch.bool, device=dev)
+    want[20:cu[1], hq // hkv:] = True
+    assert torch.equal(torch.isnan(o32).all(-1), want) and torch.equal(torch.isnan(o32).any(-1), want)
+    # (the LSE of a row with no finite scores says nothing, in any view: inputs are finite)
+    assert bool(torch.isfinite(lse.T[~want]).all())
+    v.close()
