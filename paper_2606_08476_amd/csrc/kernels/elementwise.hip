@@ -164,6 +164,9 @@ __global__ __launch_bounds__(256) void bwd_reduce_kernel(const int32_t* __restri
 
 // Largest squared row norms per head (launch_norms): D / 8 lanes a row, four rows in
 // flight per lane, a maximum per head in LDS and one per head and block written out.
+// Bound by its reads: the keys of 131K tokens and 8 heads of 128 (268 MB, some of it
+// still in the last-level cache) in 26 us; 37 us for q and k of 32 heads of 128 over
+// 64K tokens and 8 ranks.
 template <int D>
 __global__ __launch_bounds__(1024) void norm_kernel(float* norms, const u16* q, const u16* kl,
                                                     const u16* kr, int32_t t_q, int32_t t_r, int32_t hq,
