@@ -396,16 +396,17 @@ class View:
 
 
 # torch, loaded by the first call that needs it (the planners and views do not)
-torch = _Tensor = _raw_stream = BF = F32 = None
+torch = _Tensor = _raw_stream = _device = BF = F32 = None
 
 
 def _load_torch():
-    global torch, _Tensor, _raw_stream, BF, F32
+    global torch, _Tensor, _raw_stream, _device, BF, F32
     if torch is None:
         import torch as t
         _Tensor, BF, F32 = t.Tensor, t.bfloat16, t.float32
         # the current stream's handle without a Stream object, where torch has it
         raw, dev = getattr(t._C, "_cuda_getCurrentRawStream", None), getattr(t._C, "_cuda_getDevice", None)
+        _device = dev if dev is not None else t.cuda.current_device
         if raw is not None and dev is not None:
             _raw_stream = lambda: raw(dev())  # noqa: E731
         else:
@@ -642,11 +643,14 @@ class Rope:
 
 
 def _row_device(view):
-    """The device of a call on rows: the current one, which has to be the view's."""
+    """The device of a call on rows: the current one, which has to be the view's; -1
+    of a view that is not bound (which the call then refuses)."""
     if torch is None:
         _load_torch()
-    dev = torch.cuda.current_device() if view.meta is not None else -1
-    if view.meta is not None and view.meta.get_device() != dev:
+    if view.meta is None:
+        return -1
+    dev = _device()
+    if view.meta.get_device() != dev:
         raise ValueError(f"the view is bound on device {view.meta.get_device()}, the current one is {dev}")
     return dev
 
@@ -654,12 +658,12 @@ def _row_device(view):
 def _row_ptr(t, shape, dtype, name, dev):
     """(address, row stride) of a [T, H, d] tensor whose rows may lie apart."""
     if isinstance(t, _Tensor) and t.dtype is dtype and t.shape == shape and t.is_cuda:
-        if dev >= 0 and t.get_device() != dev:
+        if t.get_device() != dev and dev >= 0:
             raise ValueError(f"{name} is on device {t.get_device()}, the current one is {dev}")
+        if t.is_contiguous():
+            return t.data_ptr(), 0
         s0, s1, s2 = t.stride()
         n, h, d = shape
-        if n <= 1 and t.is_contiguous():
-            return t.data_ptr(), 0
         if s2 == 1 and (s1 == d or h == 1) and s0 >= h * d:
             return t.data_ptr(), s0
         raise ValueError(f"{name} must have whole rows: strides {(s0, s1, s2)}")
@@ -673,8 +677,7 @@ def _rows(src, dst, shape, dtype, out_dtype, name, dev):
         return None
     if src is None or dst is None:
         raise ValueError(f"{name} and its output must be given together")
-    return _ROWS.pack(*_row_ptr(src, shape, dtype, name, dev),
-                      *_row_ptr(dst, shape, out_dtype, name + "'s output", dev))
+    return _ROWS.pack(*_row_ptr(src, shape, dtype, name, dev), *_row_ptr(dst, shape, out_dtype, name, dev))
 
 
 _ROWS = struct.Struct("PqPq")
