@@ -446,3 +446,52 @@ def test_nothing_is_out_of_reach_of_a_nan(dev):  # noqa: F811
     # (the LSE of a row with no finite scores says nothing, in any view: inputs are finite)
     assert bool(torch.isfinite(lse.T[~want]).all())
     v.close()
+
+
+def test_norms_follow_the_inputs(dev):  # noqa: F811
+    """A captured forward and backward that leave keys out of reach, replayed after their
+    inputs have grown (more keys are then within reach), and the same on two streams at
+    once, each with a workspace of its own: the eager bits."""
+    r = Run("split_g4", "steep", dev)
+    v = r.view
+    fws, bws, _ = v.workspace_size()
+    assert fws >= 256 * 4 * (r.case.hq + 2 * r.case.hkv)
+    u8 = lambda m: torch.empty(m, dtype=torch.uint8, device=dev)  # noqa: E731
+
+    def calls(out, w1, w2):
+        o, o32, l, *g = out
+        F.fc_attn_fwd(v, r.q, *r.kv, 0.0, F.FC_TWO_PASS, o, o32, l, w1)
+        F.fc_attn_bwd(v, r.q, *r.kv, o, l, r.do, 0.0, *g, w2, o_f32=o32)
+
+    def outs():
+        return [r.nan(r.tq, r.case.hq, r.case.d, dt=BF), r.nan(r.tq, r.case.hq, r.case.d),
+                r.nan(r.case.hq, r.tq), *r.grads()]
+
+    got, w = outs(), (u8(fws), u8(bws))
+    calls(got, *w)
+    torch.cuda.synchronize()
+    graph = torch.cuda.CUDAGraph()
+    with torch.cuda.graph(graph):
+        calls(got, *w)
+    for grow in (1.0, 8.0, 4.0):
+        r.q.mul_(grow)
+        r.kv[2].mul_(grow)  # (received keys)
+        want = outs()
+        calls(want, u8(fws), u8(bws))
+        torch.cuda.synchronize()
+        assert all(bool(torch.isfinite(t).all()) for t in want)
+        for t in got:
+            t.fill_(float("nan"))
+        graph.replay()
+        torch.cuda.synchronize()
+        assert all(torch.equal(a, b) for a, b in zip(want, got))
+        side = [torch.cuda.Stream() for _ in range(2)]
+        both = [(outs(), u8(fws), u8(bws)) for _ in side]
+        torch.cuda.synchronize()
+        for s, b in zip(side, both):
+            with torch.cuda.stream(s):
+                calls(*b)
+        torch.cuda.synchronize()
+        for b in both:
+            assert all(torch.equal(x, y) for x, y in zip(want, b[0]))
+    v.close()
