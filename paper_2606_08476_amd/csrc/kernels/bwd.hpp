@@ -25,9 +25,10 @@ __global__ __launch_bounds__(256, D == 64 ? 3 : 2) void attn_bwd_kernel(BwdParam
 // (Scored: two waves per SIMD at 64 too, where the score's registers take 178-192 and
 // three leave 168; P's packed values not kept, as at 128 they use all 256. Against
 // views without a score function, 32/8 heads of 128 over 64K tokens and 8 ranks, capped
-// at 50: dK/dV 672 -> 777 us, dQ 467 -> 566, the whole 1133 -> 1349: bound by the issue
-// of vector instructions, 7.4 beside each MFMA and 1.5 of them transcendental, where
-// without a cap there are 3.8 and 0.6.)
+// at 50: dK/dV 672 -> 777 us, dQ 467 -> 566, the whole 1133 -> 1349: 7.4 vector
+// instructions beside each MFMA and 1.5 of them transcendental, where without a cap there
+// are 3.8 and 0.6. Neither fewer of them, r - r^2 unpacked by mixed FMAs, 16 less per
+// tile and wave, nor the score's steps a slot apart gave 1%.)
 template <int D, int HPI, int SC>
 __global__ __launch_bounds__(256, 2) void attn_bwd_scored_kernel(BwdParams p) {
   __shared__ __attribute__((aligned(16))) char smem[DkdvLds<D, false, SC>::bytes];
