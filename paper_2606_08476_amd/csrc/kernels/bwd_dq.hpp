@@ -18,8 +18,12 @@
 //
 // Scored views (SC, see score.hpp): S becomes the score before the exponential; with
 // a cap, P (r - r^2) takes P's place in dS (its 4 is in the final scale), which
-// needs no register more. A bias takes the keys' positions from LDS, copied per
-// tile by the first wave.
+// needs no register more. A bias takes the keys' positions from LDS, put there per
+// tile by the first wave, less the position of the workgroup's first row: its rows
+// follow each other in the document, so a row's own share of the bias is at most 127
+// slopes, wherever the document's rows lie. (Counted from the document's start its
+// rounding alone, half a step of slope x position, takes P out of fp32's range: at a
+// slope of 1024, from a million and a half tokens on.)
 #include "common.hpp"
 #include "launch.hpp"
 #include "score.hpp"
@@ -76,6 +80,10 @@ __device__ __forceinline__ void dq_tile(const DqParams& p, int b, char* smem) {
   };
   ranges();
   const TileLoader<D, BN, 256, BN, SC != 0> ld(p.hkv * D);
+  // BIAS: position of the workgroup's first row, from which positions are counted here;
+  // those of the next tile's keys go through a register of the first wave, a key per lane
+  const float pos0 = BIAS ? p.q_pos[q0] : 0.f;
+  float key_pos = 0.f;
   auto fetch = [&](int j, uint32_t kofs) {
     const bool rs = j < n_r;
     const int k0 = rs ? r0 + j * BN : l0 + (j - n_r) * BN;
@@ -83,11 +91,12 @@ __device__ __forceinline__ void dq_tile(const DqParams& p, int b, char* smem) {
     const size_t base = (size_t(k0) * p.hkv + kvh) * D;
     ld.load_at(lds_addr(smem) + kofs, (rs ? p.k_recv : p.k_loc) + base, hi - k0);
     ld.load_at(lds_addr(smem) + kofs + TILE, (rs ? p.v_recv : p.v_loc) + base, hi - k0);
-    if (BIAS && wave == 0) {  // and the keys' positions, a key per lane
-      const float* pos = rs ? p.recv_pos : p.q_pos;
-      lds_copy4(pos + k0, 4u * uint32_t(min(int(fresh_lane()), hi - k0 - 1)),
-                lds_addr(smem) + OP + kofs / (2 * TILE / 256));
-    }
+    if (BIAS && wave == 0)
+      key_pos = ((rs ? p.recv_pos : p.q_pos) + k0)[min(int(fresh_lane()), hi - k0 - 1)];
+  };
+  auto put_pos = [&](uint32_t kofs) {
+    if (BIAS && wave == 0)
+      *reinterpret_cast<float*>(smem + OP + kofs / (2 * TILE / 256) + 4 * fresh_lane()) = key_pos - pos0;
   };
 
   const float cap2 = p.cap2, slope2 = BIAS ? p.slopes[h] : 0.f;
@@ -110,7 +119,7 @@ __device__ __forceinline__ void dq_tile(const DqParams& p, int b, char* smem) {
   float off2 = CAP ? cap2 - lse2 : -lse2;
   if constexpr (BIAS) {
     float rest;
-    off2 = row_offset(off2, slope2, p.q_pos[min(qrow, q1 - 1)], rest);
+    off2 = row_offset(off2, slope2, p.q_pos[min(qrow, q1 - 1)] - pos0, rest);
   }
 
   // per-lane LDS byte offsets: K/V rows for k-step ks, and the two transpose
@@ -159,7 +168,10 @@ __device__ __forceinline__ void dq_tile(const DqParams& p, int b, char* smem) {
     ranges();
   }
   __syncthreads();  // every wave holds its rows before tile 0 overwrites them
-  if (n_t > 0) fetch(0, 0);
+  if (n_t > 0) {
+    fetch(0, 0);
+    put_pos(0);
+  }
   wait_async();
   __syncthreads();
 
@@ -310,6 +322,7 @@ __device__ __forceinline__ void dq_tile(const DqParams& p, int b, char* smem) {
         __builtin_amdgcn_sched_barrier(0);
       });
     }
+    if (j + 1 < n_t) put_pos(2 * TILE - KO);
     wait_async();
     __syncthreads();
   };
@@ -324,7 +337,7 @@ __device__ __forceinline__ void dq_tile(const DqParams& p, int b, char* smem) {
       const int hh = kvh * p.group + hc * HPW + l / RPW;
       const float l2 = p.lse[(size_t)hh * p.t_q + r] * kLog2e;
       float rest;
-      row_offset(CAP ? cap2 - l2 : -l2, p.slopes[hh], p.q_pos[r], rest);
+      row_offset(CAP ? cap2 - l2 : -l2, p.slopes[hh], p.q_pos[r] - pos0, rest);
       f *= __builtin_amdgcn_exp2f(rest);
     }
     return f;

@@ -19,7 +19,8 @@
 // have at most 2^24 tokens). off is large far into a document, but the sum with a
 // near key's share is exact to its own size: only the rounding of off itself is
 // left, which all scores of the row have in common. It drops out of the softmax,
-// and row_offset() gives what the row's LSE has to be corrected by.
+// and row_offset() gives what the row's LSE has to be corrected by. (dQ takes the LSE
+// as given, so nothing drops out there: it counts positions from its first row.)
 #include "common.hpp"
 #include "launch.hpp"
 

@@ -1,0 +1,127 @@
+"""Scored views whose slope times position leaves fp32's range of exponents: steep
+slopes (up to the largest a view takes) far into a document (up to the longest a view
+takes). A row's own share of its biases is then billions, of which the near keys'
+shares leave next to nothing.
+
+Keys more than a few tokens away have no weight left at such slopes (e^-745 is 0 in
+64 bits), so the oracle, and its elementwise bounds (oracle/scores.py), are those of
+the last keys alone; gradients of all others are exactly 0."""
+import numpy as np
+import pytest
+import torch
+
+from oracle import scores as S
+from paper_2606_08476_amd import flashcp as F
+from test_gpu_parity import dev, say  # noqa: F401
+
+pytestmark = pytest.mark.gpu
+
+BF, F32 = torch.bfloat16, torch.float32
+OWN, NEAR = 130, 1024  # own rows at the document's end; received keys the oracle sees
+
+
+class Far:
+    """A rank that holds the last OWN tokens of a document of n, the rest received."""
+
+    def __init__(self, dev, n, hq, hkv, d, slopes, cap, q_std, tiles):
+        cu = np.array([0, n], dtype=np.int32)
+        plan = np.array([[0, 1, 0, n - OWN], [0, 0, n - OWN, OWN]], dtype=np.int32)
+        self.view = F.View(cu, plan, 2, 0, hq, hkv, d, tiles=tiles, cap=cap, slopes=slopes).bind(dev)
+        assert (self.view.info["t_q"], self.view.info["t_recv"]) == (OWN, n - OWN)
+        self.n, self.hq, self.hkv, self.d, self.dev = n, hq, hkv, d, dev
+        g = torch.Generator(device=dev).manual_seed(n + hq + d)
+        e = lambda m, h: torch.randn(m, h, d, generator=g, device=dev, dtype=BF)  # noqa: E731
+        self.q, self.do = q_std * e(OWN, hq), e(OWN, hq)
+        self.kv = e(OWN, hkv), e(OWN, hkv), e(n - OWN, hkv), e(n - OWN, hkv)
+        doc = lambda m: torch.zeros(m, dtype=torch.int64, device=dev)  # noqa: E731
+        at = torch.arange(n - OWN - NEAR, n, device=dev)
+        k, v = (torch.cat([self.kv[2 + i][-NEAR:], self.kv[i]]) for i in (0, 1))
+        self.want, self.bound = S.attention(doc(OWN), at[NEAR:], self.q, doc(OWN + NEAR), at, k, v, cap,
+                                            slopes, self.do)
+        # (every weight that the oracle leaves out is 0 in 64 bits: a score is at most the
+        # product of two norms, here under twice 12 * 12 or the square root of d)
+        assert float(np.min(slopes)) * (NEAR - 1) > 800 + 2 * q_std * 4 * d / np.sqrt(d)
+
+    def new(self, *s, dt=F32):
+        return torch.full(s, float("nan"), dtype=dt, device=self.dev)
+
+    def grads(self):
+        m = self.n - OWN
+        return [self.new(OWN, self.hq, self.d)] + [self.new(t, self.hkv, self.d) for t in (OWN, OWN, m, m)]
+
+    def ws(self, n):
+        return torch.empty(max(n, 1), dtype=torch.uint8, device=self.dev)
+
+    def near(self, name, got, key, old=None):
+        """got within the oracle's bound; old: gradients of keys before NEAR, all 0."""
+        over = float(((got.double() - self.want[key]).abs() - self.bound[key]).max())
+        say(f"[gpu]   {name}: over its bound {over:.1e}")
+        assert bool(torch.isfinite(got).all()) and over <= 0, f"{name}: {over:.3e} over its bound"
+        if old is not None:
+            assert not bool(old.any()), f"{name}: keys without weight"
+
+
+STEEP = [
+    # tokens, heads, head dim, slopes, cap, what queries are scaled by, query tile
+    (1500003, 4, 1, 64, [1024.0, 700.0, 128.0, 1024.0], 0.0, 2.0, None),
+    (1500003, 2, 1, 128, [1024.0, 128.0], 30.0, 2.0, None),
+    (4000037, 8, 2, 128, [1024.0, 128.0, 1000.0, 333.0, 1024.0, 1024.0, 512.0, 256.0], 0.0, 2.0, None),
+    (4000037, 4, 1, 64, [1024.0, 512.0, 128.0, 64.0], 30.0, 2.0, (128, 0, 0, 0)),
+    # scores that differ by as much as the biases of neighbours: several keys matter
+    (4000037, 2, 2, 128, [1024.0, 700.0], 0.0, 800.0, None),
+    (4000037, 4, 1, 64, [128.0, 130.0, 150.0, 200.0], 600.0, 150.0, None),
+    (1 << 24, 2, 1, 64, [1024.0, 128.0], 0.0, 2.0, None),
+    (1 << 24, 2, 1, 64, [128.0, 150.0], 0.0, 150.0, None),
+]
+
+
+@pytest.mark.parametrize("n,hq,hkv,d,slopes,cap,q_std,tiles", STEEP)
+def test_gradients(n, hq, hkv, d, slopes, cap, q_std, tiles, dev):  # noqa: F811
+    """Every way to dQ, dK and dV, from the oracle's own output and LSE: deterministic
+    (with and without room for row norms), dQ alone, and by atomics."""
+    say(f"[gpu] steep gradients n={n} heads={hq}/{hkv} d={d} cap={cap}")
+    f = Far(dev, n, hq, hkv, d, np.array(slopes, dtype=np.float32), cap, q_std, tiles)
+    v, o32, lse = f.view, f.want["o"].float(), f.want["lse"].float()
+    _, bws, pws = v.workspace_size()
+    for det, short in ((True, 0), (True, 256), (False, 0)):
+        gr = f.grads()
+        F.fc_attn_bwd(v, f.q, *f.kv, None, lse, f.do, 0.0, *gr, f.ws(bws - short), deterministic=det, o_f32=o32)
+        torch.cuda.synchronize()
+        what = ("dq", "dk", "dv")
+        how = f"{'deterministic' if det else 'atomic'}{', every key' if short else ''}"
+        f.near(f"{what[0]} {how}", gr[0], "dq")
+        for name, own, got in (("dk", gr[1], gr[3]), ("dv", gr[2], gr[4])):
+            f.near(f"{name} {how}", torch.cat([got[-NEAR:], own]), name, got[:-NEAR])
+    delta, dq = f.new(hq, OWN), f.new(OWN, hq, d)
+    F.fc_bwd_preprocess(v, None, f.do, delta, o_f32=o32)
+    F.fc_attn_bwd_dq(v, f.q, *f.kv, lse, delta, f.do, 0.0, dq)
+    torch.cuda.synchronize()
+    f.near("dq alone", dq, "dq")
+    v.close()
+
+
+@pytest.mark.parametrize("n,hq,hkv,d,slopes,cap,q_std,tiles", STEEP)
+def test_forward(n, hq, hkv, d, slopes, cap, q_std, tiles, dev):  # noqa: F811
+    """Both modes, with and without room for row norms, the local partial pass, and the
+    LSE as exact as near a document's start."""
+    say(f"[gpu] steep forward n={n} heads={hq}/{hkv} d={d} cap={cap}")
+    f = Far(dev, n, hq, hkv, d, np.array(slopes, dtype=np.float32), cap, q_std, tiles)
+    v = f.view
+    for mode in (F.FC_TWO_PASS, F.FC_FUSED):
+        for short in (0, 256):
+            o, o32, lse = f.new(OWN, hq, d, dt=BF), f.new(OWN, hq, d), f.new(hq, OWN)
+            F.fc_attn_fwd(v, f.q, *f.kv, 0.0, mode, o, o32, lse, f.ws(v.workspace_size(mode)[0] - short))
+            torch.cuda.synchronize()
+            for name, got in (("o", o), ("o32", o32), ("lse", lse)):
+                bound = "o" if name == "o" else name
+                over = float(((got.double() - f.want["lse" if name == "lse" else "o"]).abs() - f.bound[bound]).max())
+                say(f"[gpu]   {name} mode {mode}{', every key' if short else ''}: over its bound {over:.1e}")
+                assert bool(torch.isfinite(got).all()) and over <= 0, f"{name}: {over:.3e} over its bound"
+    part = [f.new(OWN, hq, d), f.new(hq, OWN), f.new(OWN, hq, d), f.new(hq, OWN)]
+    F.fc_attn_fwd_partials(v, f.q, *f.kv, 0.0, *part)
+    ob, om, lm = f.new(OWN, hq, d, dt=BF), f.new(OWN, hq, d), f.new(hq, OWN)
+    F.fc_lse_merge(*part, ob, om, lm)
+    torch.cuda.synchronize()
+    assert float(((om.double() - f.want["o"]).abs() - f.bound["o32"]).max()) <= 0
+    assert float(((lm.double() - f.want["lse"]).abs() - f.bound["lse"]).max()) <= 0
+    v.close()
