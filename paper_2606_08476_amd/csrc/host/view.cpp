@@ -614,6 +614,7 @@ int build_view(const int32_t* cu, int32_t n_docs, const fc_shard* shards, int64_
         if (l > (int64_t(1) << 24))
           return fail(FC_ERR_UNSUPPORTED, "a document of a view with slopes has more than 2^24 tokens");
       v.slopes.assign(score->slopes, score->slopes + hq);
+      for (float& x : v.slopes) x += 0.f;  // (-0 becomes 0: what is divided by it has its sign)
       v.biased = true;
     } else if (v.cap > fck::kCapFixed) {
       v.slopes.assign(size_t(hq), 0.f);
