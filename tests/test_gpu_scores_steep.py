@@ -125,3 +125,26 @@ def test_forward(n, hq, hkv, d, slopes, cap, q_std, tiles, dev):  # noqa: F811
     assert float(((om.double() - f.want["o"]).abs() - f.bound["o32"]).max()) <= 0
     assert float(((lm.double() - f.want["lse"]).abs() - f.bound["lse"]).max()) <= 0
     v.close()
+
+
+def test_without_allocation(dev):  # noqa: F811
+    """A view whose plain twin fits the static scratch fits it too, however little of its
+    work is within reach, and gives the bits of a call with a workspace."""
+    n, hq, hkv, d = 16384, 8, 8, 128
+    cu = np.array([0, n], dtype=np.int32)
+    v = F.View(cu, F.fc_plan_per_doc(cu, 1), 1, 0, hq, hkv, d, slopes=np.full(hq, 0.5)).bind(dev)
+    g = torch.Generator(device=dev).manual_seed(3)
+    q, do, k, w = (torch.randn(n, h, d, generator=g, device=dev, dtype=BF) for h in (hq, hq, hkv, hkv))
+    none = torch.empty(0, hkv, d, dtype=BF, device=dev)
+    z = lambda *s, dt=F32: torch.full(s, float("nan"), dtype=dt, device=dev)  # noqa: E731
+    u8 = lambda m: torch.empty(max(m, 1), dtype=torch.uint8, device=dev)  # noqa: E731
+    fws, bws, _ = v.workspace_size(F.FC_FUSED)
+    assert bws <= F.NOALLOC_SCRATCH_BYTES
+    o, o32, lse = z(n, hq, d, dt=BF), z(n, hq, d), z(hq, n)
+    F.fc_attn_fwd(v, q, k, w, none, none, 0.0, F.FC_FUSED, o, o32, lse, u8(fws))
+    a, b = ([z(n, hq, d), z(n, hkv, d), z(n, hkv, d), z(0, hkv, d), z(0, hkv, d)] for _ in range(2))
+    F.fc_attn_bwd(v, q, k, w, none, none, o, lse, do, 0.0, *a, u8(bws), o_f32=o32)
+    F.fc_attn_bwd_noalloc(v, q, k, w, none, none, o, lse, do, 0.0, *b, o_f32=o32)
+    torch.cuda.synchronize()
+    assert all(bool(torch.isfinite(t).all()) and torch.equal(t, u) for t, u in zip(a, b))
+    v.close()
