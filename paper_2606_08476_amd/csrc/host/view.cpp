@@ -319,7 +319,11 @@ void View::build_dq_split() {
 // forward 331 us whole, 207-215 us in chunks of 32 to 128 tiles, 243 of 16; 8
 // query heads over one 4.8K-token sequence 71 -> 29 us. Grids that fill the chip
 // lose (64K whole documents: 243 us whole, 261 in chunks of 32), so the
-// estimate has to fall by 15%.
+// estimate has to fall by 15%. A view that prunes is split as if it did not: with the
+// work within reach alone in the estimate it is split more often, into chunks of
+// which most are out of reach (slopes of 0.5, 8/8 heads of 128 over 16K tokens 137
+// against 69 us, a late rank of 128K tokens, slopes of 0.25, 326 against 188), and the
+// partial passes visit every key.
 void View::build_fwd_split() {
   fwd_chunk = 0;
   partial_slots[0] = partial_slots[1] = false;
@@ -343,7 +347,7 @@ void View::build_fwd_split() {
   // a launch of more workgroups than fit ends, on average, some way into the
   // longest of the items it starts last
   auto launch_us = [&](double units, double most, int64_t sum) {
-    const double fair = wgs * (kept * double(sum) * f2 + units * wg) / kSlotsResident;
+    const double fair = wgs * (double(sum) * f2 + units * wg) / kSlotsResident;
     const double tail = units * wgs > kSlotsResident ? 0.3 * most * f1 : 0;
     return std::max(fair + tail, most * f1 + wg);
   };

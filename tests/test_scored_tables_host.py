@@ -59,3 +59,18 @@ def test_steep_slopes_take_no_more_backward_workspace(lens, cp, rank, hq, hkv, d
     a, b = plain.export_launch(), biased.export_launch()
     assert all(np.array_equal(a[k], b[k]) for k in ("bwd_launch", "bwd_reduce", "bwd_qfirst"))
     assert biased.info["n_bwd_slots"] == plain.info["n_bwd_slots"]
+
+
+@pytest.mark.parametrize("lens,cp,rank,hq,hkv,d", LAYOUTS)
+@pytest.mark.parametrize("slope", ["geometric", 0.1, 0.5, 1024.0])
+def test_steep_slopes_take_no_more_forward_workspace(lens, cp, rank, hq, hkv, d, slope):
+    """Beside the row norms, a view with slopes takes what the plain view takes, and
+    splits its key ranges as that does."""
+    s = 2.0 ** (-8.0 * np.arange(1, hq + 1) / hq) if slope == "geometric" else np.full(hq, slope)
+    plain, biased = view(lens, hq, hkv, d, cp, rank), view(lens, hq, hkv, d, cp, rank, slopes=s)
+    for mode in (F.FC_TWO_PASS, F.FC_FUSED):
+        more = biased.workspace_size(mode)[0] - plain.workspace_size(mode)[0]
+        assert more in (0, 256 * 4 * (hq + 2 * hkv))
+    a, b = plain.export_split(), biased.export_split()
+    assert a["fwd_chunk"] == b["fwd_chunk"]
+    assert all(np.array_equal(a[k], b[k]) for k in ("fwd_units", "fwd_comb"))
