@@ -209,8 +209,9 @@ typedef struct {
  * below applies it; lse is the log-sum-exp of the scores it gives, and dq, dk are
  * the gradients through it. Inputs are finite, as for every view, and with a cap and
  * no slopes values of v are below 2^36. Accuracy is that of the uncapped calls: a
- * capped score is within cap * 2^-21 of its value, and 1 - tanh^2 is rounded to fp16
- * before dK's dS is rounded to bf16.
+ * capped score is within cap * 2^-21 of its value, and 1 - tanh^2, accurate relative to
+ * its own size however far a score is beyond the cap, is rounded to 2^-11 of it (below
+ * 2^-28 to 2^-39) before dK's dS is rounded to bf16.
  * Under steep slopes most keys of a long document have no weight left. Where slopes
  * and lengths promise it, fc_attn_fwd and the backward calls that take a workspace
  * bound the scores by the rows' norms (a pass over q and k of its own; its results

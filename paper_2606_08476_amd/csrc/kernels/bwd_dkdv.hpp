@@ -34,9 +34,11 @@
 // Scored views (SC, see score.hpp): S becomes the score before the exponential, the
 // bias from the row's position and slope, which go through LDS as its LSE does.
 // With a cap dS has the factor 1 - tanh^2 = 4 (r - r^2): r - r^2 is kept beside P, as
-// fp16 (2^-11 of it, a quarter of what dS's own rounding to bf16 may be off by;
+// fp16 (2^-11 of it, an eighth of what dS's own rounding to bf16 may be off by;
 // sixteen fp32 registers more would spill), until P has been packed for dV; then W =
-// P (r - r^2) takes P's place in dS = W (dP - D), and the 4 is in the final scale.
+// P (r - r^2) takes P's place in dS = W (dP - D). It is kept times 2^16, at most 2^14,
+// so that it stays a normal fp16 number down to 2^-30 (scores of 10.4 caps, where 1 -
+// tanh^2 is 2^-28); the 4 and the 2^-16 are in the final scale.
 // P's residual is formed before that, where it is needed.
 #include "common.hpp"
 #include "launch.hpp"
@@ -186,7 +188,8 @@ __device__ __forceinline__ void dkdv_tile(const BwdParams& p, int b, char* smem)
   float row_stat = 0.f;
   // SC: cap2 goes with the rows' -LSE (put_rows)
   const float sl2 = CAP ? p.cap_in : p.scale * kLog2e, cap2 = p.cap2;
-  const float gscale = CAP ? 4.f * p.scale : p.scale;  // (W leaves out a 4)
+  constexpr int kCapLog2 = 8;  // r is formed times 2^8, r - r^2 times 2^16
+  const float gscale = CAP ? 0x1p-14f * p.scale : p.scale;  // (W is 2^16 / 4 as large)
   // position of this lane's key
   const float* const kposg = src ? p.recv_pos : p.q_pos;
   const float kpos = BIAS ? kposg[min(k0 + 32 * wave + (lane & 31), k1 - 1)] : 0.f;
@@ -301,7 +304,7 @@ __device__ __forceinline__ void dkdv_tile(const BwdParams& p, int b, char* smem)
 
     f32x16 sacc = zero16(), dpacc;
     typedef _Float16 f16x2 __attribute__((ext_vector_type(2)));
-    f16x2 rr[8];  // CAP: r - r^2
+    f16x2 rr[8];  // CAP: r - r^2, times 2^16
     float r1 = 0.f;
     bf16x8 ra[3], rb[3], pa[2], sa[2], plo[2];
     // Where P is large (short documents, keys near the diagonal) the bf16
@@ -433,13 +436,15 @@ __device__ __forceinline__ void dkdv_tile(const BwdParams& p, int b, char* smem)
           float off = SC ? le[(n - 1) & 1][e % EP] : l4[g][j];
           if constexpr (BIAS) off = __builtin_fmaf(slope2[8 * g / RPI], kpos - ce[(n - 1) & 1][e % EP], off);
           if constexpr (CAP) {
-            const float r = cap_r(sacc[e], sl2);
-            sacc[e] = __builtin_amdgcn_exp2f(__builtin_fmaf(r, -2.f * cap2, off));
-            const float r2 = __builtin_fmaf(-r, r, r);
-            if (e & 1)
+            float r2;
+            const float r = cap_r<kCapLog2>(sacc[e], sl2, r2);
+            sacc[e] = __builtin_amdgcn_exp2f(__builtin_fmaf(r, -2.f / (1 << kCapLog2) * cap2, off));
+            if (e & 1) {
               rr[e / 2] = f16x2{(_Float16)r1, (_Float16)r2};
-            else
+              asm volatile("" : "+v"(rr[e / 2]));  // here, not at its use with u and r kept
+            } else {
               r1 = r2;
+            }
           } else {
             sacc[e] = __builtin_amdgcn_exp2f(__builtin_fmaf(sacc[e], sl2, off));
           }

@@ -236,9 +236,10 @@ __device__ __forceinline__ void dq_tile(const DqParams& p, int b, char* smem) {
         float off = off2;
         if constexpr (BIAS) off = __builtin_fmaf(slope2, kp[(mb * KS + i / EP) & 1][i % EP], off);
         if constexpr (CAP) {
-          const float r = cap_r(s[mb][i], sl2);
-          s[mb][i] = __builtin_amdgcn_exp2f(__builtin_fmaf(r, -2.f * cap2, off)) *
-                     __builtin_fmaf(-r, r, r);
+          float w;
+          const float r = cap_r<0>(s[mb][i], sl2, w);
+          s[mb][i] = __builtin_amdgcn_exp2f(__builtin_fmaf(r, -2.f * cap2, off)) * w;
+          asm volatile("" : "+v"(s[mb][i]));  // here, not beyond the mask's branch with u and r kept
         } else {
           s[mb][i] = __builtin_amdgcn_exp2f(__builtin_fmaf(s[mb][i], sl2, off));
         }
