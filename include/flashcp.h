@@ -207,8 +207,9 @@ typedef struct {
  * and no slopes: fc_view_create). The view carries the function: its tables hold
  * the slopes and the positions a bias counts, and every forward and backward call
  * below applies it; lse is the log-sum-exp of the scores it gives, and dq, dk are
- * the gradients through it. Inputs are finite, as for every view, and with a cap and
- * no slopes values of v are below 2^36. Accuracy is that of the uncapped calls: a
+ * the gradients through it. Inputs are finite, as for every view, and with a cap
+ * (up to 55) and no slopes values of v are below 2^36; those under 2^-26 may lose bits in
+ * rows whose every score is near -cap. Accuracy is that of the uncapped calls: a
  * capped score is within cap * 2^-21 of its value, and 1 - tanh^2, accurate relative to
  * its own size however far a score is beyond the cap, is rounded to 2^-11 of it (below
  * 2^-28 to 2^-39) before dK's dS is rounded to bf16.
@@ -217,7 +218,7 @@ typedef struct {
  * bound the scores by the rows' norms (a pass over q and k of its own; its results
  * are the last bytes that fc_workspace_size asks for, and with less workspace every
  * key is visited) and leave out keys whose weights add up to less than 2^-76 of a
- * row's. */
+ * row's. The partial passes and fc_attn_bwd_dq, which take none, visit every key. */
 int fc_view_create_scored(const int32_t* cu_seqlens, int32_t n_docs, const fc_shard* shards,
                           int64_t n_shards, int32_t cp, int32_t rank, int32_t hq, int32_t hkv,
                           int32_t d, const fc_tile_cfg* tiles, const fc_score* score, fc_view* out);
@@ -299,10 +300,10 @@ void fc_view_destroy(fc_view view);
  * fc_attn_bwd_dkdv / fc_attn_bwd_pass take (any pointer may be NULL). On a view
  * whose long key ranges are split (fc_view_export_split) that includes the
  * query tiles' partial results, and on one that leaves out keys out of a bias's
- * reach (fc_view_create_scored) the rows' norms. With a workspace too small for
- * those the calls below run the query tiles' ranges unsplit, or visit every key,
- * and the results then differ in their last bits; they are refused (FC_ERR_WORKSPACE) only with less than that
- * takes:
+ * reach (fc_view_create_scored) the rows' norms, hq + 2 hkv KB. With a workspace
+ * too small for those the calls below run the query tiles' ranges unsplit, or visit
+ * every key, and the results then differ in their last bits; they are refused
+ * (FC_ERR_WORKSPACE) only with less than that takes:
  *   fc_attn_fwd                          FC_TWO_PASS on a view that receives keys:
  *                                        the received partial O (128 rows x d
  *                                        floats per workgroup); one pass: nothing

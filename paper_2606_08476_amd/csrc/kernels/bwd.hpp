@@ -22,13 +22,17 @@ __global__ __launch_bounds__(256, D == 64 ? 3 : 2) void attn_bwd_kernel(BwdParam
   __shared__ __attribute__((aligned(16))) char smem[DkdvLds<D>::bytes];
   dkdv_tile<D, false, HPI, D == 64 ? kKeepDs : kKeepAll>(p, blockIdx.x, smem);
 }
-// (Scored: two waves per SIMD at 64 too, where the score's registers take 178-192 and
-// three leave 168; P's packed values not kept, as at 128 they use all 256. Against
-// views without a score function, 32/8 heads of 128 over 64K tokens and 8 ranks, capped
-// at 50: dK/dV 672 -> 777 us, dQ 467 -> 566, the whole 1133 -> 1349: 7.4 vector
-// instructions beside each MFMA and 1.5 of them transcendental, where without a cap there
-// are 3.8 and 0.6. Neither fewer of them, r - r^2 unpacked by mixed FMAs, 16 less per
-// tile and wave, nor the score's steps a slot apart gave 1%.)
+// (Scored: bounds for two waves per SIMD; at 64 the kernels take 157 to 168 registers,
+// which leaves three, but for cap and bias over four heads (172). P's packed values are
+// not kept, as at 128 up to 254 of 256 are taken. Against views without a score function,
+// 32/8 heads of 128 over 64K tokens and 8 ranks, capped at 50: dK/dV 679 -> 816 us, dQ 474
+// -> 587, the whole 1148 -> 1397. Beside each MFMA there are 8.0 vector instructions, 1.5
+// of them transcendental, where without a cap there are 3.8 and 0.6. Counted, the matrix
+// unit is busy 47% of the cycles and the vector unit 56%, both at once 19% (without a cap
+// 61, 33 and 17): neither is full, two waves per SIMD leave them too little of each
+// other's work to overlap. What was tried: r - r^2 unpacked by mixed FMAs, 16
+// instructions less per tile and wave, and the score's steps a slot apart; neither gave
+// 1%.)
 template <int D, int HPI, int SC>
 __global__ __launch_bounds__(256, 2) void attn_bwd_scored_kernel(BwdParams p) {
   __shared__ __attribute__((aligned(16))) char smem[DkdvLds<D, false, SC>::bytes];

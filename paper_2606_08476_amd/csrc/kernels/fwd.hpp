@@ -59,10 +59,12 @@
 // masked and take part in the row maximum; from there on scores are in log2
 // units and the scale is gone. A cap alone needs no maximum (FIXED): its third of a
 // score, the exponential, keeps its place beside the next tile's QK products, the
-// other two are beside PV. Bound by the issue of vector instructions: per MFMA 3.0
-// transcendental ones (1.0 without a cap) and 5.4 others (4.6). 32/8 heads of 128
-// over 64K tokens and 8 ranks, two passes merged / one: no score function 407 / 347 us,
-// capped 451 / 410.
+// other two are beside PV. Per MFMA there are 3.0 transcendental instructions (1.0 without
+// a cap) and 5.4 others (4.0): the vector unit is busy 62% of the cycles (42) and the
+// matrix unit 44% (55), both at once 25% (23), so that a fifth is left to neither: waits
+// within two waves per SIMD. 32/8 heads of 128 over 64K tokens and 8 ranks, two
+// passes merged / one: no score function 381 / 355 us, capped 445 / 421; with queries
+// scaled by 6, 400 / 373 and 454 / 427.
 #include "common.hpp"
 #include "launch.hpp"
 #include "score.hpp"

@@ -57,8 +57,9 @@ struct SlotGuard {
 // a row maximum. They lie from 2^(kCapTop - 2 cap2) to 2^kCapTop: for caps up to
 // kCapFixed within 2^-100 .. 2^60, whose sums and products with values from 2^-26 to
 // 2^36 are normal numbers at any length. Views with larger caps are launched as
-// biased ones, with slopes of 0 (32/8 heads of 128, 64K tokens over 8 ranks: 463 us
-// with the fixed reference, 511 with a running maximum, 555 as biased ones).
+// biased ones, with slopes of 0 (32/8 heads of 128, 64K tokens over 8 ranks, two passes
+// with queries scaled by 6: 455 us with the fixed reference, 494 with a running maximum,
+// 521 as biased ones), in the backward too (1397 us capped at 50, 1485 at 56).
 constexpr float kCapTop = 60.f, kCapFixed = 55.f;
 
 struct FwdParams {

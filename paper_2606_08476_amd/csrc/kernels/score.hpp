@@ -6,7 +6,7 @@
 // 1 / (1 + e^2y), so with u = exp2(q.k * cap_in), cap_in = 2 scale log2(e) / cap:
 //   s2 = cap2 - 2 cap2 r,  r = 1 / (1 + u),  cap2 = cap log2(e)
 // (u overflows to infinity where the score is the cap: r = 0.) It takes two
-// instructions of the quarter-rate unit and three others, and is off by about cap
+// transcendental instructions (each the issue time of two) and three others, and is off by about cap
 // * 2^-22: with the caps allowed (at most 1024) by less than the rounding of P to
 // bf16. The derivative, which the backward needs, is 1 - tanh^2 = 4 (r - r^2), taken
 // as 4 u r^2: exact relative to its own size at either end, where a difference would
@@ -108,9 +108,10 @@ __device__ __forceinline__ float score_bound(float c, float qn, float kn, float 
 // that no long workgroup starts late. One after the other, a head's rows lie 2 KB
 // apart and fewer of the memory's channels work at a time. Measured, an L2 per head /
 // in turn / farthest first: one 98K-token document, 32/8 heads of 128, slopes 2^-1/4
-// to 2^-8, forward 4101 / 2456 / 1360 us; 64K tokens of mixed documents, 8 ranks, two
-// passes 456 / 393 / 392, backward 1275 / 987 / 967, dK/dV alone 786 / 616 / 654;
-// 16/8 heads of 64, 32K tokens, cap and bias, forward 196 / 190 / 222.
+// to 2^-8, queries scaled by 3, forward 3707 / 2226 / 1157 us, backward 10720 / 6002 /
+// 3420; 64K tokens of mixed documents, 8 ranks, two passes 412 / 324 / 323, backward
+// 1235 / 937 / 918, dK/dV alone 763 / 591 / 640; 16/8 heads of 64, 32K tokens, cap and
+// bias, queries scaled by 3, forward 183 / 180 / 211, backward 500 / 404 / 371.
 template <bool BIAS, class P>
 __device__ __forceinline__ int kv_head(const P& p, int b, int per, int& rest) {
   if (BIAS && p.norms) {
