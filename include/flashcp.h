@@ -212,7 +212,8 @@ typedef struct {
  * rows whose every score is near -cap. Accuracy is that of the uncapped calls: a
  * capped score is within cap * 2^-21 of its value, and 1 - tanh^2, accurate relative to
  * its own size however far a score is beyond the cap, is rounded to 2^-11 of it (below
- * 2^-28 to 2^-39) before dK's dS is rounded to bf16.
+ * 2^-28 to 2^-39) before dK's dS is rounded to bf16; with slopes the forward's lse is
+ * within slopes[h] * position * 2^-46 more of its value.
  * Under steep slopes most keys of a long document have no weight left. Where slopes
  * and lengths promise it, fc_attn_fwd and the backward calls that take a workspace
  * bound the scores by the rows' norms (a pass over q and k of its own; its results

@@ -20,8 +20,11 @@
 // have at most 2^24 tokens). off is large far into a document, but the sum with a
 // near key's share is exact to its own size: only the rounding of off itself is
 // left, which all scores of the row have in common. It drops out of the softmax,
-// and row_offset() gives what the row's LSE has to be corrected by. (dQ takes the LSE
-// as given, so nothing drops out there: it counts positions from its first row.)
+// and row_offset() gives what the row's LSE has to be corrected by. That is up to 2^-24
+// of slope * position, scores are as large, and their roundings leave the LSE up to
+// four times 2^-24 of that off. (Counted from the workgroup's first row they would not, but
+// a row's bits would depend on its tile, and the partial passes' on the call. dQ takes
+// the LSE as given, so nothing drops out there: it does count from its first row.)
 #include "common.hpp"
 #include "launch.hpp"
 

@@ -28,7 +28,7 @@ class Far:
         plan = np.array([[0, 1, 0, n - OWN], [0, 0, n - OWN, OWN]], dtype=np.int32)
         self.view = F.View(cu, plan, 2, 0, hq, hkv, d, tiles=tiles, cap=cap, slopes=slopes).bind(dev)
         assert (self.view.info["t_q"], self.view.info["t_recv"]) == (OWN, n - OWN)
-        self.n, self.hq, self.hkv, self.d, self.dev = n, hq, hkv, d, dev
+        self.n, self.hq, self.hkv, self.d, self.dev, self.slopes = n, hq, hkv, d, dev, slopes
         g = torch.Generator(device=dev).manual_seed(n + hq + d)
         e = lambda m, h: torch.randn(m, h, d, generator=g, device=dev, dtype=BF)  # noqa: E731
         self.q, self.do = q_std * e(OWN, hq), e(OWN, hq)
@@ -44,6 +44,15 @@ class Far:
 
     def new(self, *s, dt=F32):
         return torch.full(s, float("nan"), dtype=dt, device=self.dev)
+
+    def rounding(self):
+        """What the forward's LSE may be off by beside the oracle's bound. A row's share of
+        its biases is counted from the document's start, and off by half a step of it, at
+        most 2^-24 slope n; scores are that much off, all alike, and as large, so that
+        their own rounding, the maximum's and the sum's logarithm's, and the correction's
+        are each 2^-24 of it: four at the most."""
+        s = torch.from_numpy(self.slopes).to(self.dev).double()
+        return (s * self.n * 2.0 ** -46)[:, None]
 
     def grads(self):
         m = self.n - OWN
@@ -74,6 +83,10 @@ STEEP = [
     (1 << 24, 2, 1, 64, [128.0, 150.0], 0.0, 150.0, None),
 ]
 
+# the LSE's own accuracy: products so small that theirs is no part of the bound
+SMALL = [(1500003, 2, 1, 64, [1024.0, 512.0], 0.0, 0.01, None), (1 << 24, 2, 1, 64, [1024.0, 64.0], 0.0, 0.01, None),
+         (1 << 24, 2, 2, 128, [1024.0, 700.0], 1.0, 0.01, None)]
+
 
 @pytest.mark.parametrize("n,hq,hkv,d,slopes,cap,q_std,tiles", STEEP)
 def test_gradients(n, hq, hkv, d, slopes, cap, q_std, tiles, dev):  # noqa: F811
@@ -100,10 +113,9 @@ def test_gradients(n, hq, hkv, d, slopes, cap, q_std, tiles, dev):  # noqa: F811
     v.close()
 
 
-@pytest.mark.parametrize("n,hq,hkv,d,slopes,cap,q_std,tiles", STEEP)
+@pytest.mark.parametrize("n,hq,hkv,d,slopes,cap,q_std,tiles", STEEP + SMALL)
 def test_forward(n, hq, hkv, d, slopes, cap, q_std, tiles, dev):  # noqa: F811
-    """Both modes, with and without room for row norms, the local partial pass, and the
-    LSE as exact as near a document's start."""
+    """Both modes, with and without room for row norms, and the partial passes merged."""
     say(f"[gpu] steep forward n={n} heads={hq}/{hkv} d={d} cap={cap}")
     f = Far(dev, n, hq, hkv, d, np.array(slopes, dtype=np.float32), cap, q_std, tiles)
     v = f.view
@@ -113,8 +125,8 @@ def test_forward(n, hq, hkv, d, slopes, cap, q_std, tiles, dev):  # noqa: F811
             F.fc_attn_fwd(v, f.q, *f.kv, 0.0, mode, o, o32, lse, f.ws(v.workspace_size(mode)[0] - short))
             torch.cuda.synchronize()
             for name, got in (("o", o), ("o32", o32), ("lse", lse)):
-                bound = "o" if name == "o" else name
-                over = float(((got.double() - f.want["lse" if name == "lse" else "o"]).abs() - f.bound[bound]).max())
+                bound = f.bound[name] + (f.rounding() if name == "lse" else 0.0)
+                over = float(((got.double() - f.want["lse" if name == "lse" else "o"]).abs() - bound).max())
                 say(f"[gpu]   {name} mode {mode}{', every key' if short else ''}: over its bound {over:.1e}")
                 assert bool(torch.isfinite(got).all()) and over <= 0, f"{name}: {over:.3e} over its bound"
     part = [f.new(OWN, hq, d), f.new(hq, OWN), f.new(OWN, hq, d), f.new(hq, OWN)]
@@ -123,7 +135,7 @@ def test_forward(n, hq, hkv, d, slopes, cap, q_std, tiles, dev):  # noqa: F811
     F.fc_lse_merge(*part, ob, om, lm)
     torch.cuda.synchronize()
     assert float(((om.double() - f.want["o"]).abs() - f.bound["o32"]).max()) <= 0
-    assert float(((lm.double() - f.want["lse"]).abs() - f.bound["lse"]).max()) <= 0
+    assert float(((lm.double() - f.want["lse"]).abs() - f.bound["lse"] - f.rounding()).max()) <= 0
     v.close()
 
 
