@@ -208,8 +208,8 @@ typedef struct {
  * the slopes and the positions a bias counts, and every forward and backward call
  * below applies it; lse is the log-sum-exp of the scores it gives, and dq, dk are
  * the gradients through it. Inputs are finite, as for every view, and with a cap
- * (up to 55) and no slopes values of v are below 2^36; those under 2^-26 may lose bits in
- * rows whose every score is near -cap. Accuracy is that of the uncapped calls: a
+ * (up to 55) and no slopes values of v are below 2^36 (caps up to 41: 2^(96 - 1.45 cap));
+ * those under 2^-26 may lose bits in rows whose every score is near -cap. Accuracy is that of the uncapped calls: a
  * capped score is within cap * 2^-21 of its value, and 1 - tanh^2, accurate relative to
  * its own size however far a score is beyond the cap, is rounded to 2^-11 of it (below
  * 2^-28 to 2^-39) before dK's dS is rounded to bf16; with slopes the forward's lse is

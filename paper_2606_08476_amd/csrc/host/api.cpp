@@ -3,6 +3,7 @@
 // stream.
 #include <hip/hip_runtime.h>
 
+#include <algorithm>
 #include <cmath>
 #include <cstdint>
 #include <initializer_list>
@@ -117,6 +118,7 @@ fck::FwdParams fwd_params(const View& v, const int32_t* items, int64_t n,
   p.t_q = v.t_q();
   p.t_r = v.t_recv();
   set_score(p, v, scale);
+  p.cap_top = std::min(p.cap2, fck::kCapTop);
   return p;
 }
 

@@ -91,8 +91,8 @@ struct FwdLds {
 template <int D, int HPW, int OUT, int SC>
 __device__ __forceinline__ void fwd_tile(const FwdParams& p, char* smem) {
   constexpr bool CAP = SC & kScoreCap, BIAS = SC & kScoreBias;
-  // capped scores alone lie within the cap: the reference of every row's exponentials
-  // is kCapTop below the cap, and neither maxima nor rescaling are needed
+  // capped scores alone lie within the cap: the exponentials of every row have one
+  // reference (cap_top), and neither maxima nor rescaling are needed
   constexpr bool FIXED = SC == kScoreCap;
   constexpr bool FINAL = OUT == kOutFinal, MERGED = OUT == kOutMerged, UNIT = OUT == kOutUnit;
   constexpr bool CHUNKS = OUT == kOutChunks;
@@ -239,7 +239,7 @@ __device__ __forceinline__ void fwd_tile(const FwdParams& p, char* smem) {
   // LSE of a row with sum `tot`, natural log (BIAS: and what rounding left out of the
   // row's share, from values read again rather than held across the loop)
   auto row_lse = [&](float tot) {
-    float l = (FIXED ? cap2 - kCapTop : m) + __log2f(tot);
+    float l = (FIXED ? cap2 - p.cap_top : m) + __log2f(tot);
     if constexpr (BIAS) {
       const int ln = int(fresh_lane()) & 31, r = min(q0 + wave * RPW + ln % RPW, q1 - 1);
       float rest;
@@ -544,7 +544,7 @@ __device__ __forceinline__ void fwd_tile(const FwdParams& p, char* smem) {
 #pragma unroll
           for (int e = n * EX; e < (n + 1) * EX; ++e) {
             const float y = sc[e / 16][e % 16];
-            const float x = __builtin_amdgcn_exp2f(FIXED ? __builtin_fmaf(y, -2.f * cap2, kCapTop)
+            const float x = __builtin_amdgcn_exp2f(FIXED ? __builtin_fmaf(y, -2.f * cap2, p.cap_top)
                                                    : SC  ? y - mref
                                                          : __builtin_fmaf(y, c, -mref));
             sc[e / 16][e % 16] = x;

@@ -53,13 +53,14 @@ struct SlotGuard {
   pid_t pid_ = 0;                   // of the process that made the events
 };
 
-// Forward with capped scores alone: exponentials of score - (cap2 - kCapTop), without
-// a row maximum. They lie from 2^(kCapTop - 2 cap2) to 2^kCapTop: for caps up to
-// kCapFixed within 2^-100 .. 2^60, whose sums and products with values from 2^-26 to
-// 2^36 are normal numbers at any length. Views with larger caps are launched as
-// biased ones, with slopes of 0 (32/8 heads of 128, 64K tokens over 8 ranks, two passes
-// with queries scaled by 6: 455 us with the fixed reference, 494 with a running maximum,
-// 521 as biased ones), in the backward too (1397 us capped at 50, 1485 at 56).
+// Forward with capped scores alone: exponentials of score - (cap2 - cap_top), without
+// a row maximum. cap_top is cap2 up to kCapTop, a cap of 41: the exponentials are then of
+// the score itself, 2^-cap2 to 2^cap2, and round as numbers of the cap's size. Above it,
+// and up to kCapFixed, they lie within 2^-100 .. 2^kCapTop, whose sums and products with
+// values from 2^-26 to 2^36 are normal numbers at any length. Views with larger caps are
+// launched as biased ones, with slopes of 0 (32/8 heads of 128, 64K tokens over 8 ranks,
+// two passes with queries scaled by 6: 455 us with the fixed reference, 494 with a running
+// maximum, 521 as biased ones), in the backward too (1397 us capped at 50, 1485 at 56).
 constexpr float kCapTop = 60.f, kCapFixed = 55.f;
 
 struct FwdParams {
@@ -112,6 +113,7 @@ struct FwdParams {
   // in turn (score.hpp)
   float* norms;
   const int32_t* head_order;
+  float cap_top;            // capped alone: exponent of the largest exponential
 };
 
 struct BwdParams {

@@ -117,3 +117,75 @@ def test_saturated_scores(hq, hkv, d, biased, tiles, cap, dev):  # noqa: F811
     torch.cuda.synchronize()
     near("dq alone", alone, dq, bq, tq)
     view.close()
+
+
+@pytest.mark.parametrize("lens,cp,rank,hq,hkv,d,tiles", [
+    ([1, 300, 700, 70], 2, 1, 4, 1, 64, None), ([900, 37, 1500], 4, 2, 4, 2, 128, None),
+    ([900, 37, 1500], 3, 0, 2, 2, 64, None), ([9001, 1, 70], 8, 7, 8, 1, 128, None),  # (split)
+    ([640, 129, 1, 70], 1, 0, 8, 1, 128, (64, 0, 0, 0)),
+])
+@pytest.mark.parametrize("cap", [2.0 ** -6, 0.07, 0.6, 4.0, 55.0])
+def test_lse_of_capped_scores(lens, cp, rank, hq, hkv, d, tiles, cap, dev):  # noqa: F811
+    """Within the oracle's bound however small the cap and the LSE, from every forward
+    call: the exponentials' reference, far above the scores, costs it nothing."""
+    import _cases
+    from oracle import scores as S
+    c = _cases.make_case("lse", "llama8b", lens=lens, cp=cp, rank=rank, hq=hq, hkv=hkv, d=d, plan="per_doc")
+    v = F.View(c.cu, c.plan, cp, rank, hq, hkv, d, tiles=tiles, cap=cap).bind(dev)
+    tq, tr = v.info["t_q"], v.info["t_recv"]
+    g = torch.Generator(device=dev).manual_seed(11)
+    e = lambda n, h: torch.randn(n, h, d, generator=g, device=dev, dtype=torch.bfloat16)  # noqa: E731
+    q, kv = 2 * e(tq, hq), (e(tq, hkv), e(tq, hkv), e(tr, hkv), e(tr, hkv))
+    cu = np.asarray(c.cu)
+    at = [np.asarray(a, dtype=np.int64) for a in (c.oview.q_gpos, c.oview.recv_gpos)]
+    doc = [torch.from_numpy(np.searchsorted(cu, a, side="right") - 1).to(dev) for a in at]
+    pos = [torch.from_numpy(a).to(dev) for a in at]
+
+    def oracle(srcs):
+        cat = lambda x: torch.cat([x[i] for i in srcs])  # noqa: E731
+        return S.attention(doc[0], pos[0], q, cat(doc), cat(pos), cat(kv[::2]), cat(kv[1::2]), cap)
+
+    def near(name, got, srcs):
+        want, bound = oracle(srcs)
+        some = torch.isfinite(want["lse"])
+        assert torch.equal(torch.isfinite(got), some), name
+        over = float(torch.where(some, (got.double() - want["lse"]).abs() / bound["lse"], 0.0).max())
+        say(f"[gpu]   lse cap {cap} {name}: {over:.2f} of its bound")
+        assert over <= 1, f"{name}: {over:.2f} of its bound"
+
+    z = lambda *s, dt=torch.float32: torch.full(s, float("nan"), dtype=dt, device=dev)  # noqa: E731
+    for mode in (F.FC_TWO_PASS, F.FC_FUSED):
+        lse, ws = z(hq, tq), torch.empty(max(1, v.workspace_size(mode)[0]), dtype=torch.uint8, device=dev)
+        F.fc_attn_fwd(v, q, *kv, 0.0, mode, z(tq, hq, d, dt=torch.bfloat16), None, lse, ws)
+        torch.cuda.synchronize()
+        near(f"mode {mode}", lse, (0, 1))
+    part = [z(tq, hq, d), z(hq, tq), z(tq, hq, d), z(hq, tq)]
+    F.fc_attn_fwd_partials(v, q, *kv, 0.0, *part)
+    torch.cuda.synchronize()
+    near("local", part[1], (0,))
+    if tr:
+        near("received", part[3], (1,))
+    v.close()
+
+
+@pytest.mark.parametrize("cap,top", [(0.6, 2.0 ** 90), (20.0, 2.0 ** 62), (55.0, 2.0 ** 30), (20.0, 2.0 ** -90)])
+def test_values_of_any_size_under_a_cap(cap, top, dev):  # noqa: F811
+    """The forward of values far from 1 is that of ordinary ones, scaled: exactly, for a
+    power of two."""
+    cu = np.array([0, 700, 1400], dtype=np.int32)
+    hq, hkv, d, n = 4, 2, 64, 1400
+    view = F.View(cu, F.fc_plan_per_doc(cu, 1), 1, 0, hq, hkv, d, cap=cap).bind(dev)
+    g = torch.Generator(device=dev).manual_seed(2)
+    q, k, v = (torch.randn(n, h, d, generator=g, device=dev).bfloat16() for h in (hq, hkv, hkv))
+    none = torch.empty(0, hkv, d, dtype=torch.bfloat16, device=dev)
+    res = []
+    for s in (1.0, top):
+        o32, lse = torch.empty(n, hq, d, device=dev), torch.empty(hq, n, device=dev)
+        o = torch.empty(n, hq, d, dtype=torch.bfloat16, device=dev)
+        ws = torch.empty(max(1, view.workspace_size(F.FC_FUSED)[0]), dtype=torch.uint8, device=dev)
+        F.fc_attn_fwd(view, 4 * q, k, v * s, none, none, 0.0, F.FC_FUSED, o, o32, lse, ws)
+        res.append((o32, lse))
+    torch.cuda.synchronize()
+    assert bool(torch.isfinite(res[1][0]).all()) and torch.equal(res[0][1], res[1][1])
+    assert torch.equal(res[0][0], res[1][0] / top)
+    view.close()
