@@ -131,7 +131,7 @@ __device__ __forceinline__ void dkdv_tile(const BwdParams& p, int b, char* smem)
     const float bs = src ? score_bound<SC>(c, qn, head_norm(p.norms, p.hq + p.hkv + kvh), p.cap2) : bl;
     far = (src ? p.recv_pos : p.q_pos)[k1 - 1] + reach(bs + bl, s2);
     // no row at all: zeros, with nothing read (backward of a late rank of one 98K-token
-    // document, 32/8 heads of 128, 2423 -> 2387 us; 64K tokens of mixed documents 956)
+    // document, 32/8 heads of 128, 2423 -> 2387 us; of mixed documents no slower)
     if (__builtin_amdgcn_readfirstlane(q0 >= q1 || p.q_pos[min(q0, p.t_q - 1)] > far)) {
       const int slot = it[7];
       const size_t rs = slot < 0 ? kvs : size_t(D);

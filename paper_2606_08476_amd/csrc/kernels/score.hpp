@@ -6,9 +6,9 @@
 // 1 / (1 + e^2y), so with u = exp2(q.k * cap_in), cap_in = 2 scale log2(e) / cap:
 //   s2 = cap2 - 2 cap2 r,  r = 1 / (1 + u),  cap2 = cap log2(e)
 // (u overflows to infinity where the score is the cap: r = 0.) It takes two
-// transcendental instructions (each the issue time of two) and three others, and is off by about cap
-// * 2^-22: with the caps allowed (at most 1024) by less than the rounding of P to
-// bf16. The derivative, which the backward needs, is 1 - tanh^2 = 4 (r - r^2), taken
+// transcendental instructions (each the issue time of two) and three others, and is off
+// by about cap * 2^-22: with the caps allowed (at most 1024) by less than the rounding of
+// P to bf16. The derivative, which the backward needs, is 1 - tanh^2 = 4 (r - r^2), taken
 // as 4 u r^2: exact relative to its own size at either end, where a difference would
 // leave the rounding of r alone for scores near -cap (7% off at 7 caps; against the
 // difference, one instruction more per score, a layer of 32/8 heads of 128 over 64K
