@@ -392,6 +392,59 @@ int fc_rope_bwd(fc_view view, const fc_rope* rope, int32_t out_bf16, const fc_ro
                 const fc_rows* dk_loc, const fc_rows* dv_loc, const fc_rows* dk_recv,
                 const fc_rows* dv_recv, void* stream);
 
+/* ----------------------------------------------------------------- head norms
+ * The norm of a query's or key's head, x of d values: n = (x - m) / sqrt(mean (x -
+ * m)^2 + eps), m = 0 or (centred) mean x, times (weight + offset). Then its rotation,
+ * in the same pass, rounded once. Rows and gradients as for the rotary rows above;
+ * statistics and products are fp32. */
+typedef struct {
+  const void* weight; /* device, [d] or (per_head) [heads, d]; NULL: ones */
+  int32_t w_bf16;     /* type of weight and of its gradient: bf16, else fp32 */
+  int32_t per_head;
+  int32_t centred;
+  float offset;       /* added to weight (not to NULL's ones); finite */
+  float eps;          /* finite, at least FC_NORM_EPS_MIN */
+} fc_norm;
+#define FC_NORM_EPS_MIN 5.421010862427522e-20f /* 2^-64 */
+
+/* fc_rope_fwd with q and k normalised first (q_norm, k_norm NULL: not that one; rope
+ * NULL: not rotated). One launch. No output may overlap the weights. */
+int fc_norm_rope_fwd(fc_view view, const fc_rope* rope, const fc_norm* q_norm, const fc_norm* k_norm,
+                     const fc_rows* q, const fc_rows* k, const fc_rows* v, void* stream);
+
+/* fc_kv_gather_rope with the keys normalised first. */
+int fc_kv_gather_norm_rope(fc_view view, const fc_rope* rope, const fc_norm* k_norm, const void* k_packed,
+                           const void* v_packed, int64_t t_packed, void* k_loc, void* v_loc, void* k_recv,
+                           void* v_recv, void* stream);
+
+/* The rows that the forward normalised, bf16: row r at in + r * stride (stride in
+ * elements, as in fc_rows; 0: rows without gaps), or, packed > 0, the rows of a packed
+ * tensor of that many at the tokens' positions. */
+typedef struct {
+  const void* in;
+  int64_t stride;
+  int64_t packed;
+} fc_norm_rows;
+
+/* Workspace bytes of fc_norm_rope_bwd with gradients of the weights of both norms
+ * (either may be NULL). 16-byte aligned. */
+int fc_norm_rope_workspace(fc_view view, const fc_norm* q_norm, const fc_norm* k_norm, size_t* bytes);
+
+/* fc_rope_bwd through the norms: the gradients (fp32) of q, k_loc and k_recv as
+ * fc_norm_rope_fwd and fc_kv_gather_norm_rope write them, on their way to the rows these
+ * read, which are given beside them (q_in, k_in, k_recv_in; read only where the norm
+ * is given). dw_q ([d] or [Hq, d]) and dw_k ([d] or [Hkv, d]), of the weights' type, are
+ * written, not added to: sums over the tensors given, own and received keys (zeros if
+ * none is given or has a row); NULL: not wanted. The sums are reproducible: no atomics.
+ * ws: device, as fc_norm_rope_workspace says, if any dw is wanted. Outputs may be their
+ * own gradients (in place, fp32) and overlap nothing else that is read or written. Two
+ * launches. */
+int fc_norm_rope_bwd(fc_view view, const fc_rope* rope, const fc_norm* q_norm, const fc_norm* k_norm,
+                     int32_t out_bf16, const fc_rows* dq, const fc_rows* dk_loc, const fc_rows* dv_loc,
+                     const fc_rows* dk_recv, const fc_rows* dv_recv, const fc_norm_rows* q_in,
+                     const fc_norm_rows* k_in, const fc_norm_rows* k_recv_in, void* dw_q, void* dw_k, void* ws,
+                     size_t ws_bytes, void* stream);
+
 /* Forward. Writes o (bf16 [T_q,Hq,d]), optionally o_f32 (fp32, same shape;
  * NULL to skip) and lse (fp32 [Hq,T_q]). FC_TWO_PASS runs the local and the
  * received pass (Sec. 3.2) and their log-sum-exp merge in one launch: each

@@ -23,6 +23,7 @@ SOURCES = [
     "host/api.cpp",
     "host/noalloc.cpp",
     "host/rope.cpp",
+    "host/norm.cpp",
     "kernels/attn_fwd.hip",
     "kernels/attn_fwd_cap.hip",
     "kernels/attn_fwd_bias.hip",
@@ -34,6 +35,7 @@ SOURCES = [
     "kernels/attn_bwd_dq.hip",
     "kernels/elementwise.hip",
     "kernels/rope.hip",
+    "kernels/norm.hip",
 ]
 
 FLAGS = [

@@ -33,6 +33,7 @@ EXPORTS = [
     "fc_attn_fwd_partial", "fc_attn_fwd_partials", "fc_lse_merge", "fc_attn_bwd", "fc_bwd_preprocess",
     "fc_attn_bwd_pass", "fc_attn_bwd_dkdv", "fc_attn_bwd_dq", "fc_attn_bwd_noalloc", "fc_last_error",
     "fc_rope_freqs", "fc_rope_fwd", "fc_kv_gather_rope", "fc_rope_bwd",
+    "fc_norm_rope_fwd", "fc_kv_gather_norm_rope", "fc_norm_rope_workspace", "fc_norm_rope_bwd",
 ]
 
 # bytes of the static device scratch behind fc_attn_bwd_noalloc (flashcp.h)
@@ -64,6 +65,11 @@ class Score(C.Structure):
 class RopeCfg(C.Structure):
     _fields_ = [("dim", C.c_int32), ("interleaved", C.c_int32), ("packed_pos", C.c_int32),
                 ("amplitude", C.c_float), ("inv_freq", C.c_void_p)]
+
+
+class NormCfg(C.Structure):
+    _fields_ = [("weight", C.c_void_p), ("w_bf16", C.c_int32), ("per_head", C.c_int32),
+                ("centred", C.c_int32), ("offset", C.c_float), ("eps", C.c_float)]
 
 
 class ViewInfo(C.Structure):
@@ -128,6 +134,10 @@ def _signatures():
         "fc_rope_fwd": [P, P, P, P, P, P],
         "fc_kv_gather_rope": [P, P, P, P, C.c_int64, P, P, P, P, P],
         "fc_rope_bwd": [P, P, C.c_int32, P, P, P, P, P, P],
+        "fc_norm_rope_fwd": [P] * 8,
+        "fc_kv_gather_norm_rope": [P, P, P, P, P, C.c_int64, P, P, P, P, P],
+        "fc_norm_rope_workspace": [P, P, P, C.POINTER(C.c_size_t)],
+        "fc_norm_rope_bwd": [P, P, P, P, C.c_int32] + [P] * 11 + [C.c_size_t, P],
         "fc_attn_bwd_noalloc": [P, P, P, P, P, P, P, P, P, P, C.c_float, C.c_int32, P, P, P, P,
                                 P, P],
     }
@@ -723,3 +733,125 @@ def fc_rope_bwd(view: View, rope, dq, dk_loc, dv_loc, dk_recv, dv_recv, dq_out, 
          _rows(dv_recv, dv_recv_out, KR, F32, dt, "dv_recv", dev)]
     _check(lib().fc_rope_bwd(view.handle, None if rope is None else rope._p, int(dt is BF),
                              *a, _stream()))
+
+
+# ---------------------------------------------------------------- head norms
+
+class HeadNorm:
+    """The norm of a query's or key's head (fc_norm): its values, less their mean if
+    ``centred``, over the root of their mean square and ``eps``, times ``weight`` +
+    ``offset``. ``weight``: a device tensor [d] or [heads, d], bf16 or fp32, read by every
+    call, so that an optimiser may update it in place; None: ones, no gradient."""
+
+    def __init__(self, weight=None, eps: float = 1e-6, offset: float = 0.0, centred: bool = False):
+        if torch is None:
+            _load_torch()
+        if weight is not None:
+            if not isinstance(weight, _Tensor) or not weight.is_cuda:
+                raise TypeError("weight must be a device tensor")
+            if weight.dtype not in (BF, F32):
+                raise TypeError(f"weight must be {BF} or {F32}, got {weight.dtype}")
+            if weight.dim() not in (1, 2):
+                raise ValueError(f"weight has shape {tuple(weight.shape)}, expected [d] or [heads, d]")
+            if not weight.is_contiguous():
+                raise ValueError("weight must be contiguous")
+        self.weight, self.eps, self.offset, self.centred = weight, float(eps), float(offset), bool(centred)
+
+
+def _norm(norm, heads, d, name, dev):
+    """fc_norm of a HeadNorm (kept alive by the caller), None for None."""
+    if norm is None:
+        return None
+    w = norm.weight
+    if w is None:
+        return NormCfg(None, 0, 0, int(norm.centred), norm.offset, norm.eps)
+    if w.shape != (d,) and w.shape != (heads, d):
+        raise ValueError(f"{name} weight has shape {tuple(w.shape)}, expected {(d,)} or {(heads, d)}")
+    if not w.is_contiguous():
+        raise ValueError(f"{name} weight must be contiguous")
+    if dev >= 0 and w.get_device() != dev:
+        raise ValueError(f"{name} weight is on device {w.get_device()}, the current one is {dev}")
+    return NormCfg(w.data_ptr(), int(w.dtype is BF), int(w.dim() == 2), int(norm.centred), norm.offset,
+                   norm.eps)
+
+
+def _ref(x):
+    return None if x is None else C.addressof(x)
+
+
+def fc_norm_rope_fwd(view: View, rope, q_norm, k_norm, q, k, v, q_out, k_out, v_out):
+    """fc_rope_fwd with q and k normalised first, each by its HeadNorm (None: not
+    normalised)."""
+    dev = _row_device(view)
+    a = [_rows(q, q_out, view._q, BF, BF, "q", dev), _rows(k, k_out, view._kv, BF, BF, "k", dev),
+         _rows(v, v_out, view._kv, BF, BF, "v", dev)]
+    qn, kn = _norm(q_norm, view._q[1], view._q[2], "q", dev), _norm(k_norm, view._kv[1], view._kv[2], "k", dev)
+    _check(lib().fc_norm_rope_fwd(view.handle, None if rope is None else rope._p, _ref(qn), _ref(kn), *a,
+                                  _stream()))
+
+
+def fc_kv_gather_norm_rope(view: View, rope, k_norm, k_packed, v_packed, k_loc, v_loc, k_recv, v_recv):
+    """fc_kv_gather_rope with the keys normalised first."""
+    dev = _row_device(view)
+    for t in (k_packed, v_packed, k_loc, v_loc, k_recv, v_recv):
+        if dev >= 0 and isinstance(t, _Tensor) and t.is_cuda and t.get_device() != dev:
+            raise ValueError(f"a tensor is on device {t.get_device()}, the current one is {dev}")
+    KV, KR = view._kv, view._kvr
+    T = k_packed.shape[0]
+    packed = (T, KV[1], KV[2])
+    kn = _norm(k_norm, KV[1], KV[2], "k", dev)
+    _check(lib().fc_kv_gather_norm_rope(
+        view.handle, None if rope is None else rope._p, _ref(kn), _ptr(k_packed, packed, BF, "k_packed"),
+        _ptr(v_packed, packed, BF, "v_packed"), T, _ptr(k_loc, KV, BF, "k_loc"),
+        _ptr(v_loc, KV, BF, "v_loc"), _ptr(k_recv, KR, BF, "k_recv"), _ptr(v_recv, KR, BF, "v_recv"),
+        _stream()))
+
+
+def fc_norm_rope_workspace(view: View, q_norm, k_norm) -> int:
+    """Workspace bytes of fc_norm_rope_bwd with gradients of these norms' weights."""
+    n = C.c_size_t(0)
+    qn, kn = _norm(q_norm, view._q[1], view._q[2], "q", -1), _norm(k_norm, view._kv[1], view._kv[2], "k", -1)
+    _check(lib().fc_norm_rope_workspace(view.handle, _ref(qn), _ref(kn), C.byref(n)))
+    return n.value
+
+
+def fc_norm_rope_bwd(view: View, rope, q_norm, k_norm, dq, dk_loc, dv_loc, dk_recv, dv_recv, dq_out,
+                     dk_loc_out, dv_loc_out, dk_recv_out, dv_recv_out, q_in, k_in, k_packed,
+                     dw_q=None, dw_k=None, ws=None):
+    """fc_rope_bwd through the norms. ``q_in``, ``k_in``: the rank's own rows before their
+    norms; ``k_packed``: the packed keys, for received ones and, if ``k_in`` is None, own
+    ones. ``dw_q``, ``dw_k`` (the weights' shape and type): their gradients, written; None:
+    not wanted. ``ws``: fc_norm_rope_workspace bytes, if any is."""
+    dev = _row_device(view)
+    out = next((t for t in (dq_out, dk_loc_out, dv_loc_out, dk_recv_out, dv_recv_out) if t is not None), None)
+    dt = F32 if isinstance(out, _Tensor) and out.dtype is F32 else BF
+    Q, KV, KR = view._q, view._kv, view._kvr
+    a = [_rows(dq, dq_out, Q, F32, dt, "dq", dev), _rows(dk_loc, dk_loc_out, KV, F32, dt, "dk_loc", dev),
+         _rows(dv_loc, dv_loc_out, KV, F32, dt, "dv_loc", dev),
+         _rows(dk_recv, dk_recv_out, KR, F32, dt, "dk_recv", dev),
+         _rows(dv_recv, dv_recv_out, KR, F32, dt, "dv_recv", dev)]
+    qn, kn = _norm(q_norm, Q[1], Q[2], "q", dev), _norm(k_norm, KV[1], KV[2], "k", dev)
+
+    def given(t, shape, name, packed):
+        return None if t is None else _NORM_ROWS.pack(*_row_ptr(t, shape, BF, name, dev), packed)
+
+    T = 0 if k_packed is None else k_packed.shape[0]
+    pk = given(k_packed, (T, KV[1], KV[2]), "k_packed", T)
+    x = [given(q_in, Q, "q_in", 0), given(k_in, KV, "k_in", 0) if k_in is not None else pk, pk]
+    dws = []
+    for n, dw, name in ((q_norm, dw_q, "dw_q"), (k_norm, dw_k, "dw_k")):
+        if dw is not None:
+            w = None if n is None else n.weight
+            if w is None:
+                raise ValueError(f"{name} without weights")
+            _ptr(dw, tuple(w.shape), w.dtype, name)
+            if dev >= 0 and dw.get_device() != dev:
+                raise ValueError(f"{name} is on device {dw.get_device()}, the current one is {dev}")
+        dws.append(None if dw is None else dw.data_ptr())
+    if ws is not None and dev >= 0 and ws.get_device() != dev:
+        raise ValueError(f"ws is on device {ws.get_device()}, the current one is {dev}")
+    _check(lib().fc_norm_rope_bwd(view.handle, None if rope is None else rope._p, _ref(qn), _ref(kn),
+                                  int(dt is BF), *a, *x, *dws, *_ws(ws), _stream()))
+
+
+_NORM_ROWS = struct.Struct("Pqq")
