@@ -224,6 +224,42 @@ int fc_view_create_scored(const int32_t* cu_seqlens, int32_t n_docs, const fc_sh
                           int64_t n_shards, int32_t cp, int32_t rank, int32_t hq, int32_t hkv,
                           int32_t d, const fc_tile_cfg* tiles, const fc_score* score, fc_view* out);
 
+/* Windows: a query sees the last `window` tokens of its document up to itself, and the
+ * document's first `sinks` tokens (up to itself). */
+typedef struct {
+  int32_t window; /* 0: every earlier token */
+  int32_t sinks;  /* 0 or more; 0 without a window */
+} fc_window;
+
+/* fc_view_create_scored (score NULL: no score function) with a window (NULL: none). The
+ * view's receive set is what its queries see: every call below that fills, reads or
+ * writes received rows takes them so. Key tiles out of every row's window are visited by
+ * no call; the partial passes see the window's part of their source (a row without any:
+ * O = 0, LSE = -inf). fc_plan_stats and the planners know nothing of windows. A window
+ * with slopes does not look for keys out of the bias's reach. Where every document ends
+ * within the window of its last row here, the view is the one without a window. */
+int fc_view_create_windowed(const int32_t* cu_seqlens, int32_t n_docs, const fc_shard* shards,
+                            int64_t n_shards, int32_t cp, int32_t rank, int32_t hq, int32_t hkv,
+                            int32_t d, const fc_tile_cfg* tiles, const fc_score* score,
+                            const fc_window* window, fc_view* out);
+
+/* A view's window and sinks as given, 0 without (any pointer may be NULL). */
+int fc_view_get_window(fc_view view, int32_t* window, int32_t* sinks);
+
+/* The window tables a view's kernels read (for checks; copies of the uploaded blob):
+ * whether there are any, and then (any may be NULL)
+ *   win[t_q*4]                            per row: its window's first local and first
+ *                                         received key, the ends of its document's local
+ *                                         and received sinks (without a row that misses
+ *                                         a key: the document's first keys);
+ *   wave_end[n_bwd_launch*(bn_bwd/32)*2]  per launch item and 32-key wave: the first
+ *                                         query rows of the document that do not see its
+ *                                         first, its last key any more (2^31 - 1: sinks).
+ * In a windowed view forward items and chunks keep their ranges; of a range's tiles of
+ * bn_fwd keys those that no row of the query tile sees are left out. Sinks have backward
+ * items of their own. */
+int fc_view_export_window(fc_view view, int32_t* windowed, int32_t* win, int32_t* wave_end);
+
 /* A view's cap (0: none), whether it has slopes, and these (host, hq values, 0
  * without; any pointer may be NULL). */
 int fc_view_get_score(fc_view view, float* cap, int32_t* biased, float* slopes);

@@ -6,6 +6,7 @@ Test infrastructure only (see the package docstring).
 For query g and key u of one document, u <= g (positions in the document; query
 head h on KV head h // (Hq / Hkv)):
 
+* with a window W and S sinks, of these u only those with g - u < W or u < S;
 * x = scale <q_gh, k_uj>; s = cap tanh(x / cap) (or x, cap 0) - slope_h (g - u);
 * LSE = ln sum_u e^s, P = e^(s - LSE), O = sum_u P v_uj;
 * dP = <dO, v>, D = <dO, O>, dX = P (dP - D) (1 - tanh^2(x / cap)),
@@ -34,7 +35,7 @@ TINY = 2.0 ** (-126 + 20 + 20)
 
 
 def attention(doc_q, pos_q, q, doc_k, pos_k, k, v, cap=0.0, slopes=None, dout=None, scale=None,
-              delta_from_bf16=False):
+              delta_from_bf16=False, window=0, sinks=0):
     """(out, bounds): dicts of fp64 tensors o [T, Hq, d], lse [Hq, T] and, with dout,
     dq, dk, dv; doc_*, pos_*: int tensors, each token's document and position in it.
     Rows without a visible key: o 0, lse -inf. bounds["o32"]: of an fp32 O."""
@@ -53,6 +54,8 @@ def attention(doc_q, pos_q, q, doc_k, pos_k, k, v, cap=0.0, slopes=None, dout=No
         rows, keys = torch.nonzero(doc_q == n).flatten(), torch.nonzero(doc_k == n).flatten()
         dist = pos_q[rows][:, None] - pos_k[keys][None]
         seen = dist >= 0
+        if window:
+            seen = seen & ((dist < window) | (pos_k[keys] < sinks)[None])
         dist = dist.to(f64)
         for h in range(hq):
             Q, K, V = q[rows, h].to(f64), k[keys, h // G].to(f64), v[keys, h // G].to(f64)

@@ -28,10 +28,18 @@ SOURCES = [
     "kernels/attn_fwd_cap.hip",
     "kernels/attn_fwd_bias.hip",
     "kernels/attn_fwd_cap_bias.hip",
+    "kernels/attn_fwd_window.hip",
+    "kernels/attn_fwd_window_cap.hip",
+    "kernels/attn_fwd_window_bias.hip",
+    "kernels/attn_fwd_window_cap_bias.hip",
     "kernels/attn_bwd.hip",
     "kernels/attn_bwd_cap.hip",
     "kernels/attn_bwd_bias.hip",
     "kernels/attn_bwd_cap_bias.hip",
+    "kernels/attn_bwd_window.hip",
+    "kernels/attn_bwd_window_cap.hip",
+    "kernels/attn_bwd_window_bias.hip",
+    "kernels/attn_bwd_window_cap_bias.hip",
     "kernels/attn_bwd_dq.hip",
     "kernels/elementwise.hip",
     "kernels/rope.hip",

@@ -82,7 +82,7 @@ bool split_dq(const View& v, const void* ws, size_t ws_bytes) {
   return v.n_dq_slots && ws && ws_bytes >= pass_ws(v);
 }
 
-// A scored view's function for a kernel's parameters: cap_in takes a product to
+// A scored or windowed view's function for a kernel's parameters: cap_in takes a product to
 // twice its angle over the cap in log2 units, cap2 is the cap in those.
 template <class P>
 void set_score(P& p, const View& v, float scale) {
@@ -97,6 +97,7 @@ void set_score(P& p, const View& v, float scale) {
     p.q_pos = m + v.off.q_pos;
     p.recv_pos = m + v.off.recv_pos;
   }
+  if (v.windowed) p.win = v.dev_meta + v.off.win;
 }
 
 fck::FwdParams fwd_params(const View& v, const int32_t* items, int64_t n,
@@ -171,6 +172,7 @@ fck::BwdParams bwd_params(const View& v, const void* q, const void* k_loc, const
   p.items = m + v.off.bwd_launch;
   p.lim = m + v.off.lim;
   p.qfirst = m + v.off.bwd_qfirst;
+  if (v.windowed) p.wave_end = m + v.off.bwd_end;
   p.n_items = int32_t(v.bwd_launch.size() / 8);
   p.part_k = static_cast<float*>(ws);
   p.part_v = part ? reinterpret_cast<float*>(static_cast<char*>(ws) + part / 2) : nullptr;

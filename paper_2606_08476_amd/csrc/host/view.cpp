@@ -60,6 +60,54 @@ std::vector<int32_t> lpt_order(const std::vector<int64_t>& cost) {
 
 }  // namespace
 
+// First row of segment s whose window begins behind key k of source src (the segment's
+// end if there is none).
+int32_t View::first_row_beyond(int32_t s, int src, int32_t k) const {
+  int32_t lo = q_cu[s], hi = q_cu[s + 1];
+  while (lo < hi) {
+    const int32_t mid = lo + (hi - lo) / 2;
+    if (win[4 * size_t(mid) + size_t(src)] > k)
+      hi = mid;
+    else
+      lo = mid + 1;
+  }
+  return lo;
+}
+
+// Each row's window in key indices: a row at position p sees its document's keys at
+// positions above p - window, up to its own, and those below `sinks`. Both lists are in
+// the order of their positions, so that a window is a range of each, which does not move
+// back from row to row. A document that ends within the window of its last row has no
+// sinks but what every row sees anyway.
+void View::build_window(const int32_t* cu) {
+  win.clear();
+  windowed = false;
+  if (!window) return;
+  win.resize(4 * q_gpos.size());
+  pairs_loc = pairs_recv = 0;
+  for (size_t s = 0; s < seg_doc.size(); ++s) {
+    const int32_t c0 = cu[seg_doc[s]], s0 = q_cu[s], s1 = q_cu[s + 1], r0 = recv_cu[s], r1 = recv_cu[s + 1];
+    const bool cut = q_gpos[size_t(s1) - 1] - c0 >= window;
+    windowed = windowed || cut;
+    int32_t lo[2] = {s0, r0}, end[2] = {s0, r0};
+    if (cut) {
+      while (end[0] < s1 && q_gpos[size_t(end[0])] - c0 < sinks) ++end[0];
+      while (end[1] < r1 && recv_gpos[size_t(end[1])] - c0 < sinks) ++end[1];
+    }
+    for (int32_t i = s0; i < s1; ++i) {
+      const int64_t from = int64_t(q_gpos[size_t(i)]) - window;  // (the window is behind it)
+      while (q_gpos[size_t(lo[0])] <= from) ++lo[0];
+      while (lo[1] < lim[size_t(i)] && recv_gpos[size_t(lo[1])] <= from) ++lo[1];
+      if (!cut) lo[0] = s0, lo[1] = r0;
+      const int32_t row[4] = {lo[0], lo[1], end[0], end[1]};
+      std::copy(row, row + 4, &win[4 * size_t(i)]);
+      pairs_loc += i + 1 - lo[0] + std::max(0, std::min(end[0], lo[0]) - s0);
+      pairs_recv += lim[size_t(i)] - lo[1] + std::max(0, std::min(end[1], lo[1]) - r0);
+    }
+  }
+  if (!windowed) win.clear();
+}
+
 void View::build_tiles() {
   const int32_t S = int32_t(seg_doc.size());
   auto ldiag_of = [&](int32_t s0, int32_t t0) {
@@ -89,13 +137,26 @@ void View::build_tiles() {
       push8(fwd_fused, {t0, t1, r0, r0 + np, s0, t1, ldiag_of(s0, t0), s});
     }
   }
-  // backward, key-major: local key tiles then received key tiles
+  // backward, key-major: local key tiles then received key tiles. A windowed
+  // document's sinks, which every later row sees, have tiles of their own, before the
+  // others, whose rows end with the window of their last key.
+  auto sink_end = [&](int32_t s, int src) {
+    return windowed ? win[4 * size_t(q_cu[s]) + 2 + src] : src ? recv_cu[s] : q_cu[s];
+  };
+  auto tile_end = [&](int32_t k0, int32_t end, int32_t sink) {
+    return std::min(k0 + bn_bwd, k0 < sink ? sink : end);
+  };
+  auto rows_end = [&](int32_t s, int src, int32_t k1) {
+    const int32_t s1 = q_cu[s + 1];
+    return windowed && k1 > sink_end(s, src) ? first_row_beyond(s, src, k1 - 1) : s1;
+  };
   for (int32_t s = 0; s < S; ++s) {
     const int32_t s0 = q_cu[s], s1 = q_cu[s + 1];
-    for (int32_t k0 = s0; k0 < s1; k0 += bn_bwd) {
-      const int32_t k1 = std::min(k0 + bn_bwd, s1);
+    for (int32_t k0 = s0, k1; k0 < s1; k0 = k1) {
+      k1 = tile_end(k0, s1, sink_end(s, 0));
+      const int32_t q1 = rows_end(s, 0, k1);
       // rows i >= k0 see key k0; rows i >= k1-1 see the whole tile
-      push8(bwd, {k0, k1, k0, s1, first_tile_at_or_after(k0, s1, bm_bwd, k1 - 1), 0, s, 0});
+      push8(bwd, {k0, k1, k0, q1, first_tile_at_or_after(k0, q1, bm_bwd, k1 - 1), 0, s, 0});
     }
   }
   for (int32_t s = 0; s < S; ++s) {
@@ -103,8 +164,9 @@ void View::build_tiles() {
     const int32_t rl = recv_cu[s], rh = recv_cu[s + 1];
     // the segment's pieces in local order have non-decreasing n_P
     const int32_t pa = seg_piece[s], pb = seg_piece[s + 1];
-    for (int32_t k0 = rl; k0 < rh; k0 += bn_bwd) {
-      const int32_t k1 = std::min(k0 + bn_bwd, rh);
+    for (int32_t k0 = rl, k1; k0 < rh; k0 = k1) {
+      k1 = tile_end(k0, rh, sink_end(s, 1));
+      const int32_t q1 = rows_end(s, 1, k1);
       int32_t q0 = s1, qa = s1;
       for (int32_t p = pa; p < pb; ++p) {
         const int32_t lim_p = rl + pieces[5 * p + 4];
@@ -114,7 +176,7 @@ void View::build_tiles() {
           break;
         }
       }
-      push8(bwd, {k0, k1, q0, s1, first_tile_at_or_after(q0, s1, bm_bwd, qa), 1, s, 0});
+      push8(bwd, {k0, k1, q0, q1, first_tile_at_or_after(q0, q1, bm_bwd, qa), 1, s, 0});
     }
   }
   decide_prune();
@@ -123,7 +185,7 @@ void View::build_tiles() {
     std::vector<int64_t> c(items.size() / 8);
     for (size_t i = 0; i < c.size(); ++i) {
       const int32_t* it = &items[8 * i];
-      c[i] = ceil_div(it[3] - it[2], bn_fwd) + ceil_div(it[5] - it[4], bn_fwd);
+      c[i] = keys_of(it, 1).n + keys_of(it, 0).n;
     }
     return c;
   };
@@ -209,6 +271,16 @@ void View::build_bwd_launch() {
       bwd_qfirst.push_back(qf);
     }
   }
+  bwd_end.clear();
+  for (size_t i = 0; windowed && i < bwd_launch.size() / 8; ++i) {
+    const int32_t* it = &bwd_launch[8 * i];
+    const bool sink = it[0] < win[4 * size_t(q_cu[it[6]]) + 2 + it[5]];
+    for (int32_t w = 0; w < bn_bwd / 32; ++w) {
+      const int32_t kw = std::min(it[0] + 32 * w, it[1] - 1), kl = std::min(kw + 31, it[1] - 1);
+      bwd_end.push_back(sink ? fck::kAlways : first_row_beyond(it[6], it[5], kw));
+      bwd_end.push_back(sink ? fck::kAlways : first_row_beyond(it[6], it[5], kl));
+    }
+  }
 }
 
 // Split the key range of query tiles whose dQ workgroup would be the critical
@@ -250,7 +322,7 @@ void View::build_dq_split() {
   int32_t longest = 0;
   for (size_t i = 0; i < n; ++i) {
     const int32_t* it = &fwd_fused[8 * i];
-    tiles[i] = ceil_div(it[3] - it[2], bn_fwd) + ceil_div(it[5] - it[4], bn_fwd);
+    tiles[i] = keys_of(it, 1).n + keys_of(it, 0).n;
     total += tiles[i];
     longest = std::max(longest, tiles[i]);
   }
@@ -287,7 +359,8 @@ void View::build_dq_split() {
   std::vector<int64_t> cost;
   for (size_t i = 0; i < n; ++i) {
     const int32_t* it = &fwd_fused[8 * i];
-    const int32_t n_r = ceil_div(it[3] - it[2], bn_fwd), k = ceil_div(tiles[i], per);
+    const fck::KeyTiles kr = keys_of(it, 1), kl = keys_of(it, 0);
+    const int32_t n_r = kr.n, k = ceil_div(tiles[i], per);
     if (k > 1)
       dq_comb.insert(dq_comb.end(), {it[0], it[1], n_dq_slots, k, 0, 0, 0, 0});
     for (int32_t j = 0; j < k; ++j) {
@@ -295,11 +368,14 @@ void View::build_dq_split() {
       const int32_t a = int32_t(int64_t(tiles[i]) * j / k), b = int32_t(int64_t(tiles[i]) * (j + 1) / k);
       const int32_t ra = std::min(a, n_r), rb = std::min(b, n_r);
       const int32_t la = std::max(a, n_r) - n_r, lb = std::max(b, n_r) - n_r;
-      items.insert(items.end(), {it[0], it[1], std::min(it[2] + ra * bn_fwd, it[3]),
-                                 std::min(it[2] + rb * bn_fwd, it[3]),
-                                 std::min(it[4] + la * bn_fwd, it[5]),
-                                 std::min(it[4] + lb * bn_fwd, it[5]), it[6],
-                                 k > 1 ? n_dq_slots++ : -1});
+      // (from the first tile taken to behind the last; the kernel leaves out what is between)
+      auto cut = [&](const fck::KeyTiles& t, int32_t from, int32_t to, int32_t base, int32_t end) {
+        const int32_t x = std::min(base + (from < to ? t.at(from) : to ? t.at(to - 1) + 1 : 0) * bn_fwd, end);
+        return std::make_pair(x, from < to ? std::min(base + (t.at(to - 1) + 1) * bn_fwd, end) : x);
+      };
+      const auto [r_a, r_b] = cut(kr, ra, rb, it[2], it[3]);
+      const auto [l_a, l_b] = cut(kl, la, lb, it[4], it[5]);
+      items.insert(items.end(), {it[0], it[1], r_a, r_b, l_a, l_b, it[6], k > 1 ? n_dq_slots++ : -1});
       cost.push_back(b - a);
     }
   }
@@ -338,8 +414,8 @@ void View::build_fwd_split() {
   std::vector<int32_t> tiles(2 * n);  // per item: received, local key tiles
   for (size_t i = 0; i < n; ++i) {
     const int32_t* it = &fwd_fused[8 * i];
-    tiles[2 * i] = ceil_div(it[3] - it[2], bn_fwd);
-    tiles[2 * i + 1] = ceil_div(it[5] - it[4], bn_fwd);
+    tiles[2 * i] = keys_of(it, 1).n;
+    tiles[2 * i + 1] = keys_of(it, 0).n;
     const int32_t t = tiles[2 * i] + tiles[2 * i + 1];
     total += t;
     longest = std::max(longest, t);
@@ -399,18 +475,26 @@ void View::build_fwd_split() {
   fwd_comb.reserve(8 * n);
   for (size_t i = 0; i < n; ++i) {
     const int32_t* it = &fwd_fused[8 * i];
-    fwd_comb.insert(fwd_comb.end(), {it[0], it[1], int32_t(cost.size()), ceil_div(it[3] - it[2], len),
-                                     ceil_div(it[5] - it[4], len), 0, 0, 0});
-    for (int32_t a = it[2]; a < it[3]; a += len) {
-      const int32_t b = std::min(a + len, it[3]);
-      items.insert(items.end(), {it[0], it[1], a, b, 0, 0, 0, int32_t(cost.size())});
-      cost.push_back(ceil_div(b - a, bn_fwd));
+    int32_t made[2] = {0, 0};
+    const int32_t first = int32_t(cost.size());
+    for (int src = 1; src >= 0; --src) {
+      const fck::KeyTiles t = keys_of(it, src);
+      const int32_t base = it[src ? 2 : 4], end = it[src ? 3 : 5];
+      for (int32_t c = 0; base + c * len < end; ++c) {
+        // (a chunk that this tile's windows pass over is none of its; one that begins in
+        // what they pass over, where they come down)
+        const int32_t k0 = t.before(c * chunk), k1 = t.before((c + 1) * chunk);
+        if (k0 == k1) continue;
+        const int32_t a = base + t.at(k0) * bn_fwd, b = std::min(base + (c + 1) * len, end);
+        if (src)
+          items.insert(items.end(), {it[0], it[1], a, b, 0, 0, 0, int32_t(cost.size())});
+        else
+          items.insert(items.end(), {it[0], it[1], 0, 0, a, b, it[6], int32_t(cost.size())});
+        cost.push_back(k1 - k0);
+        ++made[src];
+      }
     }
-    for (int32_t a = it[4]; a < it[5]; a += len) {
-      const int32_t b = std::min(a + len, it[5]);
-      items.insert(items.end(), {it[0], it[1], 0, 0, a, b, it[6], int32_t(cost.size())});
-      cost.push_back(ceil_div(b - a, bn_fwd));
-    }
+    fwd_comb.insert(fwd_comb.end(), {it[0], it[1], first, made[1], made[0], 0, 0, 0});
   }
   for (int32_t i : lpt_order(cost))
     fwd_units.insert(fwd_units.end(), &items[8 * size_t(i)], &items[8 * size_t(i)] + 8);
@@ -426,7 +510,7 @@ void View::build_fwd_split() {
 void View::decide_prune() {
   prune = far_first = false;
   kept = 1;
-  if (!biased || hq > fck::kNormHeads) return;
+  if (!biased || windowed || hq > fck::kNormHeads) return;
   const double bound = 2 * 1.4427 * std::sqrt(double(d)) + 100;
   std::vector<double> far(static_cast<size_t>(hkv));
   for (int32_t g = 0; g < hkv; ++g) {
@@ -531,6 +615,14 @@ int View::check_tables() const {
     return bad("segment", size_t(n_seg));
   for (size_t i = 0; i < lim.size(); ++i)
     if (!(0 <= lim[i] && lim[i] <= tr)) return bad("receive limit", i);
+  if (win.size() != (windowed ? 4 * size_t(tq) : 0) || bwd_end.size() != (windowed ? 2 * bwd_qfirst.size() : 0))
+    return bad("window table", 0);
+  for (int32_t i = 0; i < int32_t(win.size() / 4); ++i) {
+    const int32_t* w = &win[4 * size_t(i)];
+    if (!(0 <= w[0] && w[0] <= i && 0 <= w[1] && w[1] <= lim[size_t(i)] && 0 <= w[2] && w[2] <= tq && 0 <= w[3] &&
+          w[3] <= tr))
+      return bad("window", size_t(i));
+  }
   return FC_OK;
 }
 
@@ -589,12 +681,16 @@ void View::build_meta() {
                      [&](int32_t a, int32_t b) { return least[size_t(a)] < least[size_t(b)]; });
     off.head_order = put(order);
   }
+  if (windowed) {
+    off.win = put(win);
+    off.bwd_end = put(bwd_end);
+  }
   if (meta.empty()) meta.resize(64, 0);
 }
 
 int build_view(const int32_t* cu, int32_t n_docs, const fc_shard* shards, int64_t n_shards,
                int32_t cp, int32_t rank, int32_t hq, int32_t hkv, int32_t d,
-               const fc_tile_cfg* tiles, const fc_score* score, View& v) {
+               const fc_tile_cfg* tiles, const fc_score* score, const fc_window* window, View& v) {
   std::vector<int64_t> lens;
   if (int rc = doc_lengths(cu, n_docs, lens)) return rc;
   if (int rc = validate_plan(lens, cp, shards, n_shards, false)) return rc;
@@ -628,6 +724,13 @@ int build_view(const int32_t* cu, int32_t n_docs, const fc_shard* shards, int64_
     } else if (v.cap > fck::kCapFixed) {
       v.slopes.assign(size_t(hq), 0.f);
     }
+  }
+  if (window) {
+    if (window->window < 0 || window->sinks < 0)
+      return fail(FC_ERR_INVALID_ARG, "window and sinks must be 0 or more");
+    if (window->sinks && !window->window) return fail(FC_ERR_INVALID_ARG, "sinks without a window");
+    v.window = window->window;
+    v.sinks = window->sinks;
   }
   // tile shapes: the forward / dQ query tile is 128 / (heads per workgroup)
   // rows, each of the 4 waves taking a quarter of them for every head; the
@@ -673,8 +776,11 @@ int build_view(const int32_t* cu, int32_t n_docs, const fc_shard* shards, int64_
       int32_t b = a + mine[i].len;
       ++i;
       while (i < mine.size() && mine[i].doc == doc && mine[i].offset == b) b += mine[i++].len;
-      for (int32_t u = held_end; u < a; ++u) v.recv_gpos.push_back(c0 + u);
-      gap_total += a - held_end;
+      // (windowed: of the tokens between, those that this piece's first row sees)
+      const int32_t near = v.window ? int32_t(std::max<int64_t>(held_end, int64_t(a) - v.window + 1)) : held_end;
+      for (int32_t u = held_end; u < std::min(near, v.sinks); ++u) v.recv_gpos.push_back(c0 + u);
+      for (int32_t u = near; u < a; ++u) v.recv_gpos.push_back(c0 + u);
+      gap_total += std::max(0, std::min(near, v.sinks) - held_end) + a - near;
       const int32_t qs = int32_t(v.q_gpos.size());
       for (int32_t u = a; u < b; ++u) v.q_gpos.push_back(c0 + u);
       const int32_t qe = int32_t(v.q_gpos.size());
@@ -699,6 +805,10 @@ int build_view(const int32_t* cu, int32_t n_docs, const fc_shard* shards, int64_
     }
     return f;
   };
+  v.build_window(cu);
+  // (the backward counts a row's entry of the window table in 32 bits)
+  if (v.windowed && v.t_q() > (1 << 28))
+    return fail(FC_ERR_UNSUPPORTED, "a windowed view has more than 2^28 rows");
   v.first_q = firsts(v.t_q(), 0);
   v.first_r = firsts(v.t_recv(), 1);
   if (!v.slopes.empty()) {
@@ -724,15 +834,16 @@ using namespace fc;
 
 extern "C" {
 
-int fc_view_create_scored(const int32_t* cu, int32_t n_docs, const fc_shard* shards,
-                          int64_t n_shards, int32_t cp, int32_t rank, int32_t hq, int32_t hkv,
-                          int32_t d, const fc_tile_cfg* tiles, const fc_score* score, fc_view* out) {
+int fc_view_create_windowed(const int32_t* cu, int32_t n_docs, const fc_shard* shards,
+                            int64_t n_shards, int32_t cp, int32_t rank, int32_t hq, int32_t hkv,
+                            int32_t d, const fc_tile_cfg* tiles, const fc_score* score,
+                            const fc_window* window, fc_view* out) {
   clear_error();
   if (!out) return fail(FC_ERR_INVALID_ARG, "out is null");
   *out = nullptr;
   try {
     std::unique_ptr<View> v(new View());
-    if (int rc = build_view(cu, n_docs, shards, n_shards, cp, rank, hq, hkv, d, tiles, score, *v))
+    if (int rc = build_view(cu, n_docs, shards, n_shards, cp, rank, hq, hkv, d, tiles, score, window, *v))
       return rc;
     *out = reinterpret_cast<fc_view>(v.release());
     return FC_OK;
@@ -741,11 +852,40 @@ int fc_view_create_scored(const int32_t* cu, int32_t n_docs, const fc_shard* sha
   }
 }
 
+int fc_view_create_scored(const int32_t* cu, int32_t n_docs, const fc_shard* shards,
+                          int64_t n_shards, int32_t cp, int32_t rank, int32_t hq, int32_t hkv,
+                          int32_t d, const fc_tile_cfg* tiles, const fc_score* score, fc_view* out) {
+  return fc_view_create_windowed(cu, n_docs, shards, n_shards, cp, rank, hq, hkv, d, tiles, score,
+                                 nullptr, out);
+}
+
 int fc_view_create(const int32_t* cu, int32_t n_docs, const fc_shard* shards, int64_t n_shards,
                    int32_t cp, int32_t rank, int32_t hq, int32_t hkv, int32_t d,
                    const fc_tile_cfg* tiles, fc_view* out) {
-  return fc_view_create_scored(cu, n_docs, shards, n_shards, cp, rank, hq, hkv, d, tiles, nullptr,
-                               out);
+  return fc_view_create_windowed(cu, n_docs, shards, n_shards, cp, rank, hq, hkv, d, tiles, nullptr,
+                                 nullptr, out);
+}
+
+int fc_view_get_window(fc_view view, int32_t* window, int32_t* sinks) {
+  clear_error();
+  if (!view) return fail(FC_ERR_INVALID_ARG, "view is null");
+  const View& v = *reinterpret_cast<View*>(view);
+  if (window) *window = v.window;
+  if (sinks) *sinks = v.sinks;
+  return FC_OK;
+}
+
+int fc_view_export_window(fc_view view, int32_t* windowed, int32_t* win, int32_t* wave_end) {
+  clear_error();
+  if (!view || !windowed) return fail(FC_ERR_INVALID_ARG, "null argument");
+  const View& v = *reinterpret_cast<View*>(view);
+  *windowed = v.windowed;
+  auto cp = [&](int32_t* dst, int64_t off, size_t n) {
+    if (dst) std::copy(v.meta.begin() + off, v.meta.begin() + off + int64_t(n), dst);
+  };
+  cp(win, v.off.win, v.win.size());
+  cp(wave_end, v.off.bwd_end, v.bwd_end.size());
+  return FC_OK;
 }
 
 int fc_view_get_score(fc_view view, float* cap, int32_t* biased, float* slopes) {

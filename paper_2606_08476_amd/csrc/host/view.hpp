@@ -28,6 +28,20 @@ struct View {
     return prune ? size_t(hq + 2 * hkv) * fck::kNormParts * sizeof(float) : 0;
   }
 
+  // window and sinks as given (0: no window); whether any row does not see some earlier
+  // key, and then 4 per local row: first local, first received key in its window, end of
+  // its document's local, received sinks (where no row misses a key: the first key)
+  int32_t window = 0, sinks = 0;
+  bool windowed = false;
+  std::vector<int32_t> win;
+  // a query tile's key tiles of one source (1: received)
+  fck::KeyTiles keys_of(const int32_t* it, int src) const {
+    const int32_t base = it[src ? 2 : 4], end = it[src ? 3 : 5];
+    if (!windowed) return fck::key_tiles(base, end, base, base);
+    const int32_t* w = &win[4 * size_t(it[0])];
+    return fck::key_tiles(base, end, w[src], w[2 + src]);
+  }
+
   std::vector<int32_t> q_gpos, recv_gpos;   // global positions, local / receive order
   std::vector<float> q_pos, recv_pos;       // with slopes: positions in the document
   std::vector<int32_t> seg_doc, q_cu, recv_cu, seg_piece;
@@ -50,6 +64,9 @@ struct View {
   int32_t n_bwd_slots = 0;
   // per launch item, per 32-key wave: first query row that sees its first key
   std::vector<int32_t> bwd_qfirst;
+  // windowed: per launch item and 32-key wave, the first query rows that do not see its
+  // first, its last key any more
+  std::vector<int32_t> bwd_end;
   // dQ work of the one-launch backward where long key ranges are split over
   // workgroups (empty: the fused forward items are taken whole): items in
   // launch order, last field the partial slot or -1, and one entry per split
@@ -79,6 +96,8 @@ struct View {
     int64_t seg, first_q, first_r;
     // with slopes only: fp32, slopes in log2 units; KV heads, least steep first
     int64_t slopes, q_pos, recv_pos, head_order;
+    // windowed only
+    int64_t win, bwd_end;
   } off{};
   const int32_t* dev_meta = nullptr;        // set by fc_view_bind
   // a split view's own slots, behind the tables in the bound buffer (null: the
@@ -94,6 +113,8 @@ struct View {
   void build_dq_split();
   void build_fwd_split();
   void decide_prune();
+  void build_window(const int32_t* cu);
+  int32_t first_row_beyond(int32_t s, int src, int32_t k) const;
   int32_t head_chunks() const { return hq / hkv / heads_per_tile; }
   // backward workspace: delta, the split key tiles' partial dK/dV, the split
   // query tiles' partial dQ
@@ -122,6 +143,6 @@ struct View {
 
 int build_view(const int32_t* cu, int32_t n_docs, const fc_shard* shards, int64_t n_shards,
                int32_t cp, int32_t rank, int32_t hq, int32_t hkv, int32_t d,
-               const fc_tile_cfg* tiles, const fc_score* score, View& v);
+               const fc_tile_cfg* tiles, const fc_score* score, const fc_window* window, View& v);
 
 }  // namespace fc

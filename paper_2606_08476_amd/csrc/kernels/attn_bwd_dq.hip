@@ -22,12 +22,20 @@ __global__ __launch_bounds__(256, 2) void attn_bwd_dq_scored_kernel(DqParams p) 
   dq_tile<D, HPW, D == 64 && HPW != 4, SC>(p, blockIdx.x, smem);
 }
 
+template <int D, int HPW, int KIND>
+__global__ __launch_bounds__(256, 2) void attn_bwd_dq_window_kernel(DqParams p) {
+  __shared__ __attribute__((aligned(16))) char smem[DqLds<D, KIND>::bytes];
+  dq_tile<D, HPW, D == 64 && HPW != 4, KIND>(p, blockIdx.x, smem);
+}
+
 template <int D, int SC>
 static hipError_t launch_dq_d(const DqParams& p, int hpw, hipStream_t s) {
   const dim3 grid(unsigned(p.n_items) * p.hkv * p.head_chunks), block(256);
   auto go = [&](auto w) {
     constexpr int W = decltype(w)::value;
-    if constexpr (SC)
+    if constexpr (SC & kWindow)
+      hipLaunchKernelGGL((attn_bwd_dq_window_kernel<D, W, SC>), grid, block, 0, s, p);
+    else if constexpr (SC)
       hipLaunchKernelGGL((attn_bwd_dq_scored_kernel<D, W, SC>), grid, block, 0, s, p);
     else
       hipLaunchKernelGGL((attn_bwd_dq_kernel<D, W>), grid, block, 0, s, p);
@@ -50,12 +58,8 @@ static hipError_t launch_dq_sc(const DqParams& p, int d, int hpw, hipStream_t s)
 
 hipError_t launch_bwd_dq(const DqParams& p, int d, int heads_per_tile, hipStream_t s) {
   if (p.n_items == 0) return hipSuccess;
-  switch (score_kind(p.cap2, p.slopes)) {
-    case 0: return launch_dq_sc<0>(p, d, heads_per_tile, s);
-    case kScoreCap: return launch_dq_sc<kScoreCap>(p, d, heads_per_tile, s);
-    case kScoreBias: return launch_dq_sc<kScoreBias>(p, d, heads_per_tile, s);
-    default: return launch_dq_sc<kScoreCap | kScoreBias>(p, d, heads_per_tile, s);
-  }
+  return with_kind(score_kind(p.cap2, p.slopes, p.win),
+                   [&](auto k) { return launch_dq_sc<decltype(k)::value>(p, d, heads_per_tile, s); });
 }
 
 // dQ of a query tile whose key range was split: the parts' slots added in

@@ -95,10 +95,14 @@ hipError_t launch_fwd_combine(const FwdParams& p, int d, int hpw, hipStream_t s)
 }
 
 template hipError_t launch_fwd_sc<0>(const FwdParams&, int, int, int, hipStream_t);
-// (in attn_fwd_cap.hip, attn_fwd_bias.hip and attn_fwd_cap_bias.hip)
+// (in attn_fwd_cap.hip, attn_fwd_bias.hip, attn_fwd_cap_bias.hip, and the same of windows)
 extern template hipError_t launch_fwd_sc<1>(const FwdParams&, int, int, int, hipStream_t);
 extern template hipError_t launch_fwd_sc<2>(const FwdParams&, int, int, int, hipStream_t);
 extern template hipError_t launch_fwd_sc<3>(const FwdParams&, int, int, int, hipStream_t);
+extern template hipError_t launch_fwd_sc<4>(const FwdParams&, int, int, int, hipStream_t);
+extern template hipError_t launch_fwd_sc<5>(const FwdParams&, int, int, int, hipStream_t);
+extern template hipError_t launch_fwd_sc<6>(const FwdParams&, int, int, int, hipStream_t);
+extern template hipError_t launch_fwd_sc<7>(const FwdParams&, int, int, int, hipStream_t);
 
 hipError_t launch_fwd(const FwdParams& p, int d, int heads_per_tile, bool final_out,
                       hipStream_t s) {
@@ -122,12 +126,8 @@ hipError_t launch_fwd(const FwdParams& p, int d, int heads_per_tile, bool final_
     const hipError_t e = launch_norms(p.norms, nullptr, p.k_loc, p.k_recv, p.t_q, p.t_r, p.hq, p.hkv, d, s);
     if (e != hipSuccess) return e;
   }
-  switch (score_kind(p.cap2, p.slopes)) {
-    case 0: return launch_fwd_sc<0>(p, d, heads_per_tile, out, s);
-    case kScoreCap: return launch_fwd_sc<kScoreCap>(p, d, heads_per_tile, out, s);
-    case kScoreBias: return launch_fwd_sc<kScoreBias>(p, d, heads_per_tile, out, s);
-    default: return launch_fwd_sc<kScoreCap | kScoreBias>(p, d, heads_per_tile, out, s);
-  }
+  return with_kind(score_kind(p.cap2, p.slopes, p.win),
+                   [&](auto k) { return launch_fwd_sc<decltype(k)::value>(p, d, heads_per_tile, out, s); });
 }
 
 }  // namespace fck

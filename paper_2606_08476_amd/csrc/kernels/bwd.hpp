@@ -39,6 +39,16 @@ __global__ __launch_bounds__(256, 2) void attn_bwd_scored_kernel(BwdParams p) {
   dkdv_tile<D, false, HPI, kKeepDs, SC>(p, blockIdx.x, smem);
 }
 
+// (Windows with slopes at head dim 128, and capped with dQ by atomics for ungrouped heads,
+// take 257 registers and more: one wave per SIMD instead of two and spills.)
+template <int D, int KIND, bool MORE = false>
+constexpr int kWindowWaves = D == 128 && ((KIND & kScoreBias) || MORE) ? 1 : 2;
+template <int D, int HPI, int KIND>
+__global__ __launch_bounds__(256, (kWindowWaves<D, KIND>)) void attn_bwd_window_kernel(BwdParams p) {
+  __shared__ __attribute__((aligned(16))) char smem[DkdvLds<D, false, KIND>::bytes];
+  dkdv_tile<D, false, HPI, kKeepDs, KIND>(p, blockIdx.x, smem);
+}
+
 // The non-deterministic backward pass: key tiles only, each also adding its
 // share of dQ into p.dq (zeroed beforehand) with atomics.
 // (kKeepNone where the registers are short. Kept values spilled 4 at head dim 128
@@ -55,6 +65,13 @@ template <int D, int HPI, int SC>
 __global__ __launch_bounds__(256, 2) void attn_bwd_atomic_scored_kernel(BwdParams p) {
   __shared__ __attribute__((aligned(16))) char smem[DkdvLds<D, true, SC>::bytes];
   dkdv_tile<D, true, HPI, kKeepNone, SC>(p, blockIdx.x, smem);
+}
+
+template <int D, int HPI, int KIND>
+__global__ __launch_bounds__(256, (kWindowWaves<D, KIND, HPI == 1 && (KIND & kScoreCap)>)) void
+attn_bwd_atomic_window_kernel(BwdParams p) {
+  __shared__ __attribute__((aligned(16))) char smem[DkdvLds<D, true, KIND>::bytes];
+  dkdv_tile<D, true, HPI, kKeepNone, KIND>(p, blockIdx.x, smem);
 }
 
 // The whole backward pass in one launch: the first n_dkdv workgroups take
@@ -82,6 +99,19 @@ __global__ __launch_bounds__(256, 2) void attn_bwd_grid_scored_kernel(BwdParams 
     dq_tile<D, HPW, D == 64, SC>(dp, b - n_dkdv, smem);
 }
 
+template <int D, int HPW, int HPI, int KIND>
+__global__ __launch_bounds__(256, (kWindowWaves<D, KIND>)) void attn_bwd_grid_window_kernel(BwdParams bp,
+                                                                                         DqParams dp,
+                                                                                         int n_dkdv) {
+  constexpr uint32_t kKeys = DkdvLds<D, false, KIND>::bytes, kRows = DqLds<D, KIND>::bytes;
+  __shared__ __attribute__((aligned(16))) char smem[kKeys > kRows ? kKeys : kRows];
+  const int b = blockIdx.x;
+  if (b < n_dkdv)
+    dkdv_tile<D, false, HPI, kKeepDs, KIND>(bp, b, smem);
+  else
+    dq_tile<D, HPW, D == 64, KIND>(dp, b - n_dkdv, smem);
+}
+
 // (HPW, the dQ workgroups' heads per tile, divides the group as HPI does,
 // so HPW <= HPI)
 template <int D, int SC>
@@ -91,7 +121,9 @@ static hipError_t launch_grid_d(const BwdParams& bp, const DqParams& dp, int hpw
   const int hpi = heads_per_iteration(bp.group);
   auto go = [&](auto w, auto i) {
     constexpr int W = decltype(w)::value, I = decltype(i)::value;
-    if constexpr (SC)
+    if constexpr (SC & kWindow)
+      hipLaunchKernelGGL((attn_bwd_grid_window_kernel<D, W, I, SC>), grid, block, 0, s, bp, dp, n_dkdv);
+    else if constexpr (SC)
       hipLaunchKernelGGL((attn_bwd_grid_scored_kernel<D, W, I, SC>), grid, block, 0, s, bp, dp, n_dkdv);
     else
       hipLaunchKernelGGL((attn_bwd_grid_kernel<D, W, I>), grid, block, 0, s, bp, dp, n_dkdv);
@@ -125,19 +157,21 @@ static hipError_t launch_keys_d(const BwdParams& p, hipStream_t s) {
 template <int D, int HPI, int SC>
 struct DkdvKernel {
   static constexpr auto fn() {
-    if constexpr (SC) return attn_bwd_scored_kernel<D, HPI, SC>;
+    if constexpr (SC & kWindow) return attn_bwd_window_kernel<D, HPI, SC>;
+    else if constexpr (SC) return attn_bwd_scored_kernel<D, HPI, SC>;
     else return attn_bwd_kernel<D, HPI>;
   }
 };
 template <int D, int HPI, int SC>
 struct AtomicKernel {
   static constexpr auto fn() {
-    if constexpr (SC) return attn_bwd_atomic_scored_kernel<D, HPI, SC>;
+    if constexpr (SC & kWindow) return attn_bwd_atomic_window_kernel<D, HPI, SC>;
+    else if constexpr (SC) return attn_bwd_atomic_scored_kernel<D, HPI, SC>;
     else return attn_bwd_atomic_kernel<D, HPI>;
   }
 };
 
-// (one kind of score per source file)
+// (one kind of view per source file)
 template <int SC>
 hipError_t launch_bwd_grid_sc(const BwdParams& bp, const DqParams& dp, int d, int hpw, hipStream_t s) {
   if (d == 64) return launch_grid_d<64, SC>(bp, dp, hpw, s);

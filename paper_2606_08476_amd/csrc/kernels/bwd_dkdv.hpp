@@ -48,12 +48,14 @@
 
 namespace fck {
 
-template <int D, bool DQ = false, int SC = 0>
+template <int D, bool DQ = false, int KIND = 0>
 struct DkdvLds {
-  // -LSE/-delta/limit slots (and the rows' positions), the key tile, two
+  // -LSE/-delta/limit slots (and the rows' positions, and their windows), the key tile, two
   // Q and two dO tiles; with DQ the transposed dS tile (128 keys x 32 queries,
   // bf16) after them
-  static constexpr uint32_t stats = (SC & kScoreBias) ? 4 * 256 : 3 * 256;  // per buffer
+  static constexpr int SC = KIND & kScores;
+  static constexpr uint32_t window = (SC & kScoreBias) ? 4 * 256 : 3 * 256;
+  static constexpr uint32_t stats = window + ((KIND & kWindow) ? 256 : 0);  // per buffer
   // with DQ and a cap, at head dim 128, a sixteenth of each wave's V operands, whose
   // registers would spill
   static constexpr bool vpart = DQ && (SC & kScoreCap) && D == 128;
@@ -66,8 +68,10 @@ enum { kKeepNone = 0, kKeepDs = 1, kKeepAll = 2 };
 
 // One workgroup's key tile (workgroup index b); smem: DkdvLds<D, DQ>::bytes
 // of shared memory. HPI (1, 2 or 4) must divide the group size.
-template <int D, bool DQ, int HPI, int KEEP, int SC = 0>
+template <int D, bool DQ, int HPI, int KEEP, int KIND = 0>
 __device__ __forceinline__ void dkdv_tile(const BwdParams& p, int b, char* smem) {
+  constexpr int SC = KIND & kScores;
+  constexpr bool WIN = KIND & kWindow, LEAN = KIND != 0;
   constexpr bool CAP = SC & kScoreCap, BIAS = SC & kScoreBias;
   constexpr int BN = 128;       // keys per workgroup
   constexpr int BM = 32;        // (query row, head) pairs per iteration
@@ -79,11 +83,12 @@ __device__ __forceinline__ void dkdv_tile(const BwdParams& p, int b, char* smem)
   constexpr uint32_t QT = BM * D * 2;  // bytes of a Q or dO tile
   // LDS layout (bytes): per buffer b, -LSE in log2 units at ST*b, -delta at
   // +256, receive limits at +512 (one wave each, the first BM entries used), with a
-  // bias the rows' positions at +768; then
+  // bias the rows' positions at +768, windowed the windows' starts behind these; then
   // the key tile; then Q and dO of buffer 0 and of buffer 1. The loop is
   // unrolled by two, so every read names its buffer with a compile-time
   // offset (all below 64 KiB, the reach of the offset field).
-  constexpr uint32_t ST = DkdvLds<D, DQ, SC>::stats;
+  constexpr uint32_t ST = DkdvLds<D, DQ, KIND>::stats;
+  constexpr uint32_t SW = DkdvLds<D, DQ, KIND>::window;
   constexpr uint32_t OK = 2 * ST;
   constexpr uint32_t OQ0 = OK + KT, OO0 = OQ0 + QT, OQ1 = OO0 + QT, OO1 = OQ1 + QT;
   // dS^T tile (DQ only): row k (key) holds the tile's 32 queries, 64 bytes;
@@ -92,16 +97,16 @@ __device__ __forceinline__ void dkdv_tile(const BwdParams& p, int b, char* smem)
   // chunk) and the transpose reads (4 keys x 16 queries per 16 lanes) both
   // spread over the 64 banks
   constexpr uint32_t ODS = OO1 + QT;
-  constexpr bool VPART = DkdvLds<D, DQ, SC>::vpart;  // V's first k-step is read from LDS
+  constexpr bool VPART = DkdvLds<D, DQ, KIND>::vpart;  // V's first k-step is read from LDS
   constexpr uint32_t OVP = ODS + 128 * 32 * 2;
-  static_assert(ODS + (DQ ? 128 * 32 * 2 : 0) + (VPART ? 4096 : 0) == DkdvLds<D, DQ, SC>::bytes, "LDS layout");
+  static_assert(ODS + (DQ ? 128 * 32 * 2 : 0) + (VPART ? 4096 : 0) == DkdvLds<D, DQ, KIND>::bytes, "LDS layout");
 
   const int lane = threadIdx.x & 63, wave = wave_id();
   // the lane's index where it should not be held in a register up to here
-  auto lane_here = [&]() { return SC ? fresh_lane() : opaque(uint32_t(lane)); };
+  auto lane_here = [&]() { return LEAN ? fresh_lane() : opaque(uint32_t(lane)); };
   const int half = lane >> 5;
   int item;  // the launch list is in launch order
-  const int kvh = kv_head<BIAS>(p, b, p.n_items, item);
+  const int kvh = kv_head<BIAS && !WIN>(p, b, p.n_items, item);
   const int32_t* it = p.items + 8 * item;  // launch list
   const int k0 = it[0], k1 = it[1], q0 = it[2], qfull = it[4], src = it[5];
   int q1 = it[3];
@@ -116,11 +121,14 @@ __device__ __forceinline__ void dkdv_tile(const BwdParams& p, int b, char* smem)
   // exceeds it)
   const int kw = k0 + 32 * wave;
   const int qfirst = p.qfirst[4 * item + wave];
+  // WIN: the first rows that do not see its first, its last key any more
+  const int qcut = WIN ? p.wave_end[8 * item + 2 * wave] : kAlways;
+  const int qend = WIN ? p.wave_end[8 * item + 2 * wave + 1] : kAlways;
 
   // BIAS: rows from this position on are out of reach of the tile's last key, for every
   // head of the group: none of the tile's keys has a weight in them
   float far = INFINITY;
-  if (BIAS && p.norms) {
+  if (BIAS && !WIN && p.norms) {
     float qn = 0.f, s2 = INFINITY;
     for (int i = 0; i < p.group; ++i) {
       qn = fmaxf(qn, head_norm(p.norms, kvh * p.group + i));
@@ -158,7 +166,7 @@ __device__ __forceinline__ void dkdv_tile(const BwdParams& p, int b, char* smem)
   // V rows of this lane's key as the B operand of dP = dO V^T
   bf16x8 vreg[KS];
 
-  if (BIAS && p.norms)
+  if (BIAS && !WIN && p.norms)
     q1 = __builtin_amdgcn_readfirstlane(first_at(p.q_pos, q0, q1, nextafterf(far, INFINITY)));
   const int ntile = (q1 - q0 + RPI - 1) / RPI;
   const int n_it = ntile * (p.group / HPI);
@@ -193,7 +201,7 @@ __device__ __forceinline__ void dkdv_tile(const BwdParams& p, int b, char* smem)
   // position of this lane's key
   const float* const kposg = src ? p.recv_pos : p.q_pos;
   const float kpos = BIAS ? kposg[min(k0 + 32 * wave + (lane & 31), k1 - 1)] : 0.f;
-  const TileLoader<D, BM, 256, RPI, SC == 0 ? 0 : DQ && D == 128 ? 2 : 1> ldq(p.hq * D, D);
+  const TileLoader<D, BM, 256, RPI, !LEAN ? 0 : DQ && D == 128 ? 2 : 1> ldq(p.hq * D, D);
   auto fetch = [&](int hh, int tt, int buf) {
     const int h = kvh * p.group + hh * HPI;
     const int t0 = q0 + tt * RPI;
@@ -201,7 +209,7 @@ __device__ __forceinline__ void dkdv_tile(const BwdParams& p, int b, char* smem)
     const uint32_t sb = lds_addr(smem);
     ldq.load_at(sb + (buf ? OQ1 : OQ0), p.q + base, q1 - t0);
     ldq.load_at(sb + (buf ? OO1 : OO0), p.dout + base, q1 - t0);
-    const int m = (SC ? int(fresh_lane()) : lane) & 31;
+    const int m = (LEAN ? int(fresh_lane()) : lane) & 31;
     const uint32_t roff = 4u * uint32_t(min(t0 + m % RPI, q1 - 1));
     const uint32_t qoff = roff + 4u * uint32_t(m / RPI) * uint32_t(p.t_q);
     const uint32_t sm = sb + ST * buf;
@@ -212,6 +220,7 @@ __device__ __forceinline__ void dkdv_tile(const BwdParams& p, int b, char* smem)
       lds_copy4(p.lim, roff, sm + 512);
     }
     if (BIAS && wave == 3) lds_copy4(p.q_pos, roff, sm + 768);
+    if (WIN && wave == 2) lds_copy4(p.win + src, 4u * roff, sm + SW);
   };
   auto put_rows = [&](int buf) {
     if (wave < 2)
@@ -289,7 +298,7 @@ __device__ __forceinline__ void dkdv_tile(const BwdParams& p, int b, char* smem)
     // than held across the loop)
     const bool diag = t0 < qfull;
     const uint32_t ln = lane_here();
-    const int hf = int(ln >> 5), hrow = SC ? hf : half;
+    const int hf = int(ln >> 5), hrow = LEAN ? hf : half;
     const int kid = k0 + 32 * wave + int(ln & 31);
     const bool kval = kid < k1;
     const int hiq = q1 - t0 - 4 * hf;
@@ -382,6 +391,19 @@ __device__ __forceinline__ void dkdv_tile(const BwdParams& p, int b, char* smem)
         const int lim = !src ? 0x7fffffff
                         : j == 0 ? m4[g].x : j == 1 ? m4[g].y : j == 2 ? m4[g].z : m4[g].w;
         pv[e] = ((cq >= lo) & (cq < hiq) & (kl < lim)) ? pv[e] : 0.f;
+      }
+      if constexpr (WIN) {
+        // and where it is before the row's window (sinks never are)
+        if (t0 + RPI > qcut) {
+          #pragma unroll
+          for (int g = 0; g < 4; ++g) {
+            const int4 w4 = *reinterpret_cast<const int4*>(smem + SO + SW + 4 * (8 * g + 4 * hrow));
+            pv[4 * g] = w4.x <= kid ? pv[4 * g] : 0.f;
+            pv[4 * g + 1] = w4.y <= kid ? pv[4 * g + 1] : 0.f;
+            pv[4 * g + 2] = w4.z <= kid ? pv[4 * g + 2] : 0.f;
+            pv[4 * g + 3] = w4.w <= kid ? pv[4 * g + 3] : 0.f;
+          }
+        }
       }
     };
     // LDS operand reads of slot n into ring entry n % 3
@@ -577,8 +599,9 @@ __device__ __forceinline__ void dkdv_tile(const BwdParams& p, int b, char* smem)
     pr = opaque(pr);
     pt = opaque(pt);
     const int tlast = min(t0 + RPI, q1) - 1;
-    const bool computed = !(kw >= k1 || tlast < qfirst);
-    if (computed) tile(t0, hh, bufc, !(t0 >= qfull && t0 + RPI <= q1 && kw + 32 <= k1));
+    const bool computed = !(kw >= k1 || tlast < qfirst || (WIN && t0 >= qend));
+    if (computed)
+      tile(t0, hh, bufc, !(t0 >= qfull && t0 + RPI <= q1 && kw + 32 <= k1 && (!WIN || t0 + RPI <= qcut)));
     f32x16 qacc;
     if constexpr (DQ) {
       if (!computed) put_ds(uint4{0u, 0u, 0u, 0u}, uint4{0u, 0u, 0u, 0u});
@@ -607,14 +630,14 @@ __device__ __forceinline__ void dkdv_tile(const BwdParams& p, int b, char* smem)
     base = (size_t(slot) * p.hkv + kvh) * BN * D;
     r0 = 0;
   }
-  const int le = SC ? int(fresh_lane()) : lane;
+  const int le = LEAN ? int(fresh_lane()) : lane;
 #pragma unroll
   for (int db = 0; db < DB; ++db) {
 #pragma unroll
     for (int i = 0; i < 16; ++i) {
-      const int r = 32 * wave + 8 * (i >> 2) + 4 * (SC ? le >> 5 : half) + (i & 3);
+      const int r = 32 * wave + 8 * (i >> 2) + 4 * (LEAN ? le >> 5 : half) + (i & 3);
       if (k0 + r < k1) {
-        const size_t g = base + size_t(r0 + r) * rs + 32 * db + ((SC ? le : lane) & 31);
+        const size_t g = base + size_t(r0 + r) * rs + 32 * db + ((LEAN ? le : lane) & 31);
         outK[g] = gscale * dk[db][i];
         outV[g] = dv[db][i];
       }

@@ -32,16 +32,20 @@
 
 namespace fck {
 
-template <int D, int SC = 0>
+template <int D, int KIND = 0>
 struct DqLds {
-  // two K and two V tiles; with a bias the positions of two tiles' keys
-  static constexpr uint32_t bytes = 4 * 64 * D * 2 + ((SC & kScoreBias) ? 2 * 256 : 0);
+  // two K and two V tiles; with a bias the positions of two tiles' keys; windowed, those
+  // of the rows
+  static constexpr uint32_t bytes =
+      4 * 64 * D * 2 + ((KIND & kScoreBias) ? 2 * 256 : 0) + ((KIND & kWindow) ? kWindowLds : 0);
 };
 
 // One workgroup's query tile (workgroup index b); smem: DqLds<D>::bytes of
 // shared memory. HOLD: sixteen registers hold -D for dP's accumulators.
-template <int D, int HPW, bool HOLD, int SC = 0>
+template <int D, int HPW, bool HOLD, int KIND = 0>
 __device__ __forceinline__ void dq_tile(const DqParams& p, int b, char* smem) {
+  constexpr int SC = KIND & kScores;
+  constexpr bool WIN = KIND & kWindow, LEAN = KIND != 0;
   constexpr bool CAP = SC & kScoreCap, BIAS = SC & kScoreBias;
   constexpr int BN = 64;
   constexpr int RPW = 32 / HPW;  // query rows per wave and head
@@ -51,12 +55,13 @@ __device__ __forceinline__ void dq_tile(const DqParams& p, int b, char* smem) {
   // LDS: K0 | V0 | K1 | V1 (double buffer); the loop is unrolled by two so
   // every read names its buffer with a compile-time offset
   constexpr uint32_t OP = 4 * TILE;  // BIAS: key positions
-  static_assert(OP + (BIAS ? 512 : 0) == DqLds<D, SC>::bytes, "LDS layout");
+  constexpr uint32_t OW = OP + (BIAS ? 512 : 0);  // WIN: the rows' windows
+  static_assert(OW + (WIN ? kWindowLds : 0) == DqLds<D, KIND>::bytes, "LDS layout");
 
   const int lane = threadIdx.x & 63, wave = wave_id();
   const int half = lane >> 5;
   int rest;
-  const int kvh = kv_head<BIAS>(p, b, p.n_items * p.head_chunks, rest);
+  const int kvh = kv_head<BIAS && !WIN>(p, b, p.n_items * p.head_chunks, rest);
   const int hc = rest % p.head_chunks;
   const int32_t* it = p.items + 8 * (rest / p.head_chunks);
   const int q0 = it[0], q1 = it[1], r1 = it[3], l1 = it[5];
@@ -74,19 +79,27 @@ __device__ __forceinline__ void dq_tile(const DqParams& p, int b, char* smem) {
   const float gscale = CAP ? 4.f * p.scale : p.scale;
 
   int n_r = 0, n_t = 0;
+  WindowTiles wt{};
   auto ranges = [&]() {
-    n_r = (r1 - r0 + BN - 1) / BN;
-    n_t = n_r + (l1 - l0 + BN - 1) / BN;
+    if constexpr (WIN) wt = window_tiles(p.win, q0, q1, r0, r1, l0, l1);
+    n_r = WIN ? wt.recv.n : (r1 - r0 + BN - 1) / BN;
+    n_t = n_r + (WIN ? wt.local.n : (l1 - l0 + BN - 1) / BN);
   };
   ranges();
-  const TileLoader<D, BN, 256, BN, SC != 0> ld(p.hkv * D);
+  if constexpr (WIN) put_window(smem + OW, 32 * wave + l31, p.win, min(qrow, q1 - 1));
+  auto tile_at = [&](int j) {  // first key of the j-th tile taken
+    const bool rs = j < n_r;
+    const int t = rs ? j : j - n_r;
+    return (rs ? r0 : l0) + (WIN ? (rs ? wt.recv : wt.local).at(t) : t) * BN;
+  };
+  const TileLoader<D, BN, 256, BN, LEAN> ld(p.hkv * D);
   // BIAS: position of the workgroup's first row, from which positions are counted here;
   // those of the next tile's keys go through a register of the first wave, a key per lane
   const float pos0 = BIAS ? p.q_pos[q0] : 0.f;
   float key_pos = 0.f;
   auto fetch = [&](int j, uint32_t kofs) {
     const bool rs = j < n_r;
-    const int k0 = rs ? r0 + j * BN : l0 + (j - n_r) * BN;
+    const int k0 = tile_at(j);
     const int hi = rs ? r1 : l1;
     const size_t base = (size_t(k0) * p.hkv + kvh) * D;
     ld.load_at(lds_addr(smem) + kofs, (rs ? p.k_recv : p.k_loc) + base, hi - k0);
@@ -149,7 +162,7 @@ __device__ __forceinline__ void dq_tile(const DqParams& p, int b, char* smem) {
       oreg[ks] = lds_b128(smem, 2u * uint32_t(qb ^ (ks << 4)), 0);
     }
   }
-  if (BIAS && p.norms) {
+  if (BIAS && !WIN && p.norms) {
     // the ranges start, whole tiles on, at the first key within reach of a row of the
     // workgroup, given its LSE
     float n2 = 0.f;
@@ -189,7 +202,7 @@ __device__ __forceinline__ void dq_tile(const DqParams& p, int b, char* smem) {
     constexpr uint32_t KO = decltype(buf)::value * 2 * TILE, VO = KO + TILE;
     if (j + 1 < n_t) fetch(j + 1, 2 * TILE - KO);
     const bool rs = j < n_r;
-    const int k0 = rs ? r0 + j * BN : l0 + (j - n_r) * BN;
+    const int k0 = tile_at(j);
     const int hi = rs ? r1 : l1;
     if (active) {
 #pragma unroll
@@ -204,10 +217,11 @@ __device__ __forceinline__ void dq_tile(const DqParams& p, int b, char* smem) {
       // give P = 0. Only edge tiles (diagonal, or running past the range)
       // mask, in one branch before each half's dS.
       const bool diag = !rs && k0 >= ldiag;
-      const int ln = SC ? int(fresh_lane()) : lane, hf = SC ? ln >> 5 : half;
-      const int qr = SC ? q0 + wave * RPW + (ln & 31) % RPW : qrow;
+      const int ln = LEAN ? int(fresh_lane()) : lane, hf = LEAN ? ln >> 5 : half;
+      const int qr = LEAN ? q0 + wave * RPW + (ln & 31) % RPW : qrow;
       const int rel = (diag ? min(hi, qr + 1) : hi) - k0 - 4 * hf;
-      const bool edge = diag || k0 + BN > hi;
+      const int sink = rs ? wt.sink_r : wt.sink_l;
+      const bool edge = diag || k0 + BN > hi || (WIN && k0 < (rs ? wt.last_r : wt.last_l) && k0 + BN > sink);
 
       f32x16 s[2] = {zero16(), zero16()}, dp[2];
       bf16x8 ring[3], sb[4];
@@ -245,7 +259,13 @@ __device__ __forceinline__ void dq_tile(const DqParams& p, int b, char* smem) {
         }
       };
       auto mask = [&](int mb) {
-        if (edge) {
+        if (WIN && edge) {  // seen: in the window, or a sink
+          const int from = *reinterpret_cast<const int*>(smem + OW + 8 * (32 * wave + (ln & 31)) + (rs ? 4 : 0)) -
+                           k0 - 4 * hf;
+          const uint32_t seen = seen_keys(rel, from, sink - k0 - 4 * hf);
+#pragma unroll
+          for (int i = 0; i < 16; ++i) s[mb][i] = seen & (1u << (16 * mb + i)) ? s[mb][i] : 0.f;
+        } else if (edge) {
 #pragma unroll
           for (int i = 0; i < 16; ++i)
             s[mb][i] = 32 * mb + 8 * (i >> 2) + (i & 3) < rel ? s[mb][i] : 0.f;

@@ -82,14 +82,19 @@ enum {
   kOutChunks = 5
 };
 
-template <int D, int SC>
+template <int D, int KIND>
 struct FwdLds {
-  // two K and two V tiles; with a bias the positions of two tiles' keys
-  static constexpr uint32_t bytes = 4 * 64 * D * 2 + ((SC & kScoreBias) ? 2 * 256 : 0);
+  // two K and two V tiles; with a bias the positions of two tiles' keys; windowed, those
+  // of the rows
+  static constexpr uint32_t bytes =
+      4 * 64 * D * 2 + ((KIND & kScoreBias) ? 2 * 256 : 0) + ((KIND & kWindow) ? kWindowLds : 0);
 };
 
-template <int D, int HPW, int OUT, int SC>
+template <int D, int HPW, int OUT, int KIND>
 __device__ __forceinline__ void fwd_tile(const FwdParams& p, char* smem) {
+  constexpr int SC = KIND & kScores;
+  constexpr bool WIN = KIND & kWindow;
+  constexpr bool LEAN = KIND != 0;  // registers are short: lane's values counted where needed
   constexpr bool CAP = SC & kScoreCap, BIAS = SC & kScoreBias;
   // capped scores alone lie within the cap: the exponentials of every row have one
   // reference (cap_top), and neither maxima nor rescaling are needed
@@ -114,13 +119,14 @@ __device__ __forceinline__ void fwd_tile(const FwdParams& p, char* smem) {
   // the prologue, which therefore ends with a barrier of its own.
   // (a bias: then the positions of the keys of K0 and of K1)
   constexpr uint32_t OP = 4 * TILE;
-  static_assert(OP + (BIAS ? 512 : 0) == FwdLds<D, SC>::bytes, "LDS layout");
+  constexpr uint32_t OW = OP + (BIAS ? 512 : 0);  // WIN: the rows' windows
+  static_assert(OW + (WIN ? kWindowLds : 0) == FwdLds<D, KIND>::bytes, "LDS layout");
 
   const int lane = threadIdx.x & 63, wave = wave_id();
   const int half = lane >> 5;
   const int b = blockIdx.x;
   int rest;
-  const int kvh = kv_head<BIAS>(p, b, (UNIT ? p.n_units : p.n_items) * p.head_chunks, rest);
+  const int kvh = kv_head<BIAS && !WIN>(p, b, (UNIT ? p.n_units : p.n_items) * p.head_chunks, rest);
   const int hc = rest % p.head_chunks;
   const int32_t* it = (UNIT ? p.units : p.items) + 8 * (rest / p.head_chunks);
   const int q0 = it[0], q1 = it[1], r1 = it[3], l1 = it[5];
@@ -157,7 +163,7 @@ __device__ __forceinline__ void fwd_tile(const FwdParams& p, char* smem) {
   };
   // BIAS, final output: the ranges start, whole tiles on, at the first key within
   // reach of a row of the workgroup (the rows' norms from their registers)
-  const bool cut = BIAS && (FINAL || MERGED || (UNIT && p.o_bf16)) && p.norms;
+  const bool cut = BIAS && !WIN && (FINAL || MERGED || (UNIT && p.o_bf16)) && p.norms;
   if (cut) {
     read_q();
     float n2 = 0.f;
@@ -174,14 +180,20 @@ __device__ __forceinline__ void fwd_tile(const FwdParams& p, char* smem) {
                  qvalid ? at - reach(bl + bl, slope2) : INFINITY, r0, r1, l0, l1);
   }
 
+  // WIN: what the tile's rows see
+  WindowTiles wt{};
+  if constexpr (WIN) {
+    wt = window_tiles(p.win, q0, q1, r0, r1, l0, l1);
+    put_window(smem + OW, 32 * wave + l31, p.win, min(qrow, q1 - 1));
+  }
   // key tiles: first the received range, then the local range
-  const int n_r = (r1 - r0 + BN - 1) / BN;
-  const int n_t = n_r + (l1 - l0 + BN - 1) / BN;
+  const int n_r = WIN ? wt.recv.n : (r1 - r0 + BN - 1) / BN;
+  const int n_t = n_r + (WIN ? wt.local.n : (l1 - l0 + BN - 1) / BN);
 
   // async copy of the K (or V) rows of key tile j into the buffer at byte
   // offset `ofs`; rows past the range repeat the last row (finite data;
   // those keys are masked)
-  const TileLoader<D, BN, 256, BN, SC != 0> ld(p.hkv * D);
+  const TileLoader<D, BN, 256, BN, LEAN> ld(p.hkv * D);
   // first key of the j-th tile taken (BIAS: each source from its last tile on, or each
   // of its chunks, the nearest keys first, so that maxima seldom grow)
   auto tile_at = [&](int j) {
@@ -189,9 +201,17 @@ __device__ __forceinline__ void fwd_tile(const FwdParams& p, char* smem) {
     int t = rs ? j : j - n_r;
     if constexpr (BIAS) {
       const int n = rs ? n_r : n_t - n_r;
-      const int c0 = CHUNKS ? t & -p.chunk : 0;  // (a power of 2)
-      t = c0 + (CHUNKS ? min(p.chunk, n - c0) : n) - 1 - (t - c0);
+      if constexpr (WIN) {
+        const KeyTiles k = rs ? wt.recv : wt.local;
+        const int g = CHUNKS ? k.at(t) & -p.chunk : 0;  // (a power of 2)
+        const int c0 = CHUNKS ? k.before(g) : 0, c1 = CHUNKS ? k.before(g + p.chunk) : n;
+        t = c0 + c1 - 1 - t;
+      } else {
+        const int c0 = CHUNKS ? t & -p.chunk : 0;  // (a power of 2)
+        t = c0 + (CHUNKS ? min(p.chunk, n - c0) : n) - 1 - (t - c0);
+      }
     }
+    if constexpr (WIN) t = rs ? wt.recv.at(t) : wt.local.at(t);
     return (rs ? r0 : l0) + t * BN;
   };
   auto fetch = [&](int j, uint32_t ofs, bool v) {
@@ -318,12 +338,12 @@ __device__ __forceinline__ void fwd_tile(const FwdParams& p, char* smem) {
     // each lane with a row, side by side)
     // (lane-derived offsets from an opaque copy of the lane index: not held
     // across the key loop)
-    const int ln = SC ? int(fresh_lane()) : int(opaque(uint32_t(lane))), pr = ln & 31;
-    // (SC: what the epilogue needs of the lane's row, counted anew too)
-    const int l31_ = SC ? pr : l31, half_ = SC ? ln >> 5 : half;
-    const int h_ = SC ? kvh * p.group + hc * HPW + l31_ / RPW : h;
-    const int qrow_ = SC ? q0 + wave * RPW + l31_ % RPW : qrow;
-    const bool qvalid_ = SC ? qrow_ < q1 : qvalid;
+    const int ln = LEAN ? int(fresh_lane()) : int(opaque(uint32_t(lane))), pr = ln & 31;
+    // (LEAN: what the epilogue needs of the lane's row, counted anew too)
+    const int l31_ = LEAN ? pr : l31, half_ = LEAN ? ln >> 5 : half;
+    const int h_ = LEAN ? kvh * p.group + hc * HPW + l31_ / RPW : h;
+    const int qrow_ = LEAN ? q0 + wave * RPW + l31_ % RPW : qrow;
+    const bool qvalid_ = LEAN ? qrow_ < q1 : qvalid;
     const int nv = min(RPW, q1 - (q0 + wave * RPW));
     const int ci = 2 * ((pr / RPW) * nv + pr % RPW) + (ln >> 5);
     float* const rows = out + (size_t(q0 + wave * RPW) * p.hq + kvh * p.group + hc * HPW) * D;
@@ -386,8 +406,20 @@ __device__ __forceinline__ void fwd_tile(const FwdParams& p, char* smem) {
     m = -INFINITY;
     lsum = 0.f;
   };
-  // CHUNKS: first key tile after the current chunk
-  int chunk_end = CHUNKS ? (n_r > 0 ? min(p.chunk, n_r) : min(p.chunk, n_t)) : 0;
+  // CHUNKS: first key tile after the current chunk, the one that tile j begins (WIN: its
+  // chunk may begin before, or end behind, what is taken of it); and whether it is the
+  // source's first
+  auto next_chunk = [&](int j) {
+    if constexpr (WIN) {
+      const bool rs = j < n_r;
+      const KeyTiles k = rs ? wt.recv : wt.local;
+      const int base = rs ? 0 : n_r;
+      return base + k.before((k.at(j - base) & -p.chunk) + p.chunk);
+    }
+    return min(j + p.chunk, j < n_r ? n_r : n_t);
+  };
+  int chunk_end = CHUNKS ? next_chunk(0) : 0;
+  bool first_chunk = true;
 
   // S^T = K Q^T for the K tile at byte offset ko (prologue only; the loop
   // interleaves the same products with the softmax), two independent
@@ -410,10 +442,21 @@ __device__ __forceinline__ void fwd_tile(const FwdParams& p, char* smem) {
     const int k0 = tile_at(j);
     const int hi = rs ? r1 : l1;
     const bool diag = !rs && k0 >= ldiag;
-    if (diag || k0 + BN > hi) {
-      const int ln = SC ? int(fresh_lane()) : lane, hf = SC ? ln >> 5 : half;
-      const int qr = SC ? q0 + wave * RPW + (ln & 31) % RPW : qrow;
+    const int sink = rs ? wt.sink_r : wt.sink_l;
+    const bool cut_off = WIN && k0 < (rs ? wt.last_r : wt.last_l) && k0 + BN > sink;
+    if (diag || k0 + BN > hi || cut_off) {
+      const int ln = LEAN ? int(fresh_lane()) : lane, hf = LEAN ? ln >> 5 : half;
+      const int qr = LEAN ? q0 + wave * RPW + (ln & 31) % RPW : qrow;
       const int rel = (diag ? min(hi, qr + 1) : hi) - k0 - 4 * hf;
+      if constexpr (WIN) {
+        // seen: in the window, or a sink
+        const int from = *reinterpret_cast<const int*>(smem + OW + 8 * (32 * wave + (ln & 31)) + (rs ? 4 : 0)) -
+                         k0 - 4 * hf;
+        const uint32_t seen = seen_keys(rel, from, sink - k0 - 4 * hf);
+#pragma unroll
+        for (int n = 0; n < 32; ++n) s[n / 16][n % 16] = seen & (1u << n) ? s[n / 16][n % 16] : kHidden;
+        return;
+      }
 #pragma unroll
       for (int mb = 0; mb < 2; ++mb)
 #pragma unroll
@@ -491,8 +534,9 @@ __device__ __forceinline__ void fwd_tile(const FwdParams& p, char* smem) {
     if (CHUNKS && j == chunk_end) {
       const bool recv = j <= n_r;
       const int c0 = recv ? 0 : n_r;  // the source's first key tile
-      if (active) finish_chunk(recv, j - c0 <= p.chunk, j == n_r, false);
-      chunk_end = min(j + p.chunk, j < n_r ? n_r : n_t);
+      if (active) finish_chunk(recv, WIN ? first_chunk : j - c0 <= p.chunk, j == n_r, false);
+      first_chunk = j == n_r;
+      chunk_end = next_chunk(j);
     }
     if (active) {
       // a row's output is rescaled only when its maximum grows by more than
@@ -600,7 +644,7 @@ __device__ __forceinline__ void fwd_tile(const FwdParams& p, char* smem) {
   if constexpr (CHUNKS) {
     // the last source's partial: in oacc, normalised, after its last chunk
     const bool recv = !p.o_f32;
-    if (active) finish_chunk(recv, n_t - (recv ? 0 : n_r) <= p.chunk, true, true);
+    if (active) finish_chunk(recv, WIN ? first_chunk : n_t - (recv ? 0 : n_r) <= p.chunk, true, true);
     store_rows<D, RPW>(
         smem + size_t(wave) * (32 * D * 4), active,
         [&](int db, int g) {
@@ -689,10 +733,19 @@ __global__ __launch_bounds__(256, 2) void attn_fwd_scored_kernel(FwdParams p) {
   __shared__ __attribute__((aligned(16))) char smem[FwdLds<D, SC>::bytes];
   fwd_tile<D, HPW, OUT, SC>(p, smem);
 }
-template <int D, int HPW, int OUT, int SC>
+// (Windows with slopes at head dim 128 take 257 registers and more: one wave per SIMD
+// instead of two and spills.)
+template <int D, int HPW, int OUT, int KIND>
+__global__ __launch_bounds__(256, D == 128 && (KIND & kScoreBias) ? 1 : 2) void attn_fwd_window_kernel(FwdParams p) {
+  __shared__ __attribute__((aligned(16))) char smem[FwdLds<D, KIND>::bytes];
+  fwd_tile<D, HPW, OUT, KIND>(p, smem);
+}
+template <int D, int HPW, int OUT, int KIND>
 static void launch_fwd_kernel(const FwdParams& p, dim3 grid, hipStream_t s) {
-  if constexpr (SC)
-    hipLaunchKernelGGL((attn_fwd_scored_kernel<D, HPW, OUT, SC>), grid, dim3(256), 0, s, p);
+  if constexpr (KIND & kWindow)
+    hipLaunchKernelGGL((attn_fwd_window_kernel<D, HPW, OUT, KIND>), grid, dim3(256), 0, s, p);
+  else if constexpr (KIND)
+    hipLaunchKernelGGL((attn_fwd_scored_kernel<D, HPW, OUT, KIND>), grid, dim3(256), 0, s, p);
   else
     hipLaunchKernelGGL((attn_fwd_kernel<D, HPW, OUT>), grid, dim3(256), 0, s, p);
 }
@@ -752,7 +805,7 @@ static hipError_t launch_fwd_d(const FwdParams& p, int hpw, int out, hipStream_t
   }
 }
 
-// (one kind of score per source file)
+// (one kind of view per source file)
 template <int SC>
 hipError_t launch_fwd_sc(const FwdParams& p, int d, int hpw, int out, hipStream_t s) {
   if (d == 64) return launch_fwd_d<64, SC>(p, hpw, out, s);

@@ -63,6 +63,32 @@ struct SlotGuard {
 // maximum, 521 as biased ones), in the backward too (1397 us capped at 50, 1485 at 56).
 constexpr float kCapTop = 60.f, kCapFixed = 55.f;
 
+// Windowed views. A query tile takes a source's keys base .. end-1 in tiles of 64, but for
+// those that none of its rows sees: with `lo` the first key in the window of its first
+// row (rows' windows do not move back) and the keys before `sink` seen by every row, tiles
+// 0 .. head-1 and head+skip .. , n in all. (base is the first key, or any whole number
+// of tiles on: parts of a range leave out the same tiles.)
+struct KeyTiles {
+  int32_t head, skip, n;
+  // the tile taken i-th
+  __host__ __device__ int32_t at(int32_t i) const { return i < head ? i : i + skip; }
+  // how many of those taken come before tile t
+  __host__ __device__ int32_t before(int32_t t) const {
+    const int32_t far = t - skip > head ? t - skip : head;
+    const int32_t k = t <= head ? t : far;
+    return k < n ? k : n;
+  }
+};
+__host__ __device__ inline KeyTiles key_tiles(int32_t base, int32_t end, int32_t lo, int32_t sink) {
+  constexpr int32_t BN = 64;
+  const int32_t all = (end - base + BN - 1) / BN;
+  int32_t head = sink > base ? (sink - base + BN - 1) / BN : 0;
+  if (head > all) head = all;
+  int32_t from = lo >= end ? all : lo > base ? (lo - base) / BN : 0;
+  if (from < head) from = head;
+  return {head, from - head, all - (from - head)};
+}
+
 struct FwdParams {
   const uint16_t* q;        // [t_q, hq, d] bf16
   const uint16_t* k_recv;   // [t_r, hkv, d]
@@ -114,6 +140,10 @@ struct FwdParams {
   float* norms;
   const int32_t* head_order;
   float cap_top;            // capped alone: exponent of the largest exponential
+  // windowed views: 4 int32 per local row, the first local and the first received key in
+  // its window, and the ends of the local and received keys that its document's every
+  // row sees; null if not windowed
+  const int32_t* win;
 };
 
 struct BwdParams {
@@ -148,7 +178,12 @@ struct BwdParams {
   // in turn (score.hpp)
   float* norms;
   const int32_t* head_order;
+  // windowed views: as in FwdParams; and per item and 32-key wave the first query row
+  // that does not see its first key any more, and its last (both kAlways: no such row)
+  const int32_t* win;
+  const int32_t* wave_end;
 };
+constexpr int32_t kAlways = 0x7fffffff;
 
 struct DqParams {
   const uint16_t* q;        // [t_q, hq, d]
@@ -181,6 +216,7 @@ struct DqParams {
   // in turn (score.hpp)
   float* norms;
   const int32_t* head_order;
+  const int32_t* win;       // windowed views: as in FwdParams
 };
 
 // blocks of the norm pass: partial maxima per head

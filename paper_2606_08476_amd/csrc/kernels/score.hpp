@@ -28,12 +28,30 @@
 #include "common.hpp"
 #include "launch.hpp"
 
+#include <type_traits>
+
 namespace fck {
 
-enum { kScoreCap = 1, kScoreBias = 2 };
+// Kinds of views: what their scores are, and whether rows see windows.
+enum { kScoreCap = 1, kScoreBias = 2, kScores = 3, kWindow = 4 };
 
-inline int score_kind(float cap2, const float* slopes) {
-  return (cap2 > 0.f ? kScoreCap : 0) | (slopes ? kScoreBias : 0);
+inline int score_kind(float cap2, const float* slopes, const int32_t* win) {
+  return (cap2 > 0.f ? kScoreCap : 0) | (slopes ? kScoreBias : 0) | (win ? kWindow : 0);
+}
+// go(std::integral_constant<int, kind>())
+template <class F>
+hipError_t with_kind(int kind, const F& go) {
+  switch (kind) {
+    case 0: return go(std::integral_constant<int, 0>());
+    case 1: return go(std::integral_constant<int, 1>());
+    case 2: return go(std::integral_constant<int, 2>());
+    case 3: return go(std::integral_constant<int, 3>());
+    case 4: return go(std::integral_constant<int, 4>());
+    case 5: return go(std::integral_constant<int, 5>());
+    case 6: return go(std::integral_constant<int, 6>());
+    case 7: return go(std::integral_constant<int, 7>());
+    default: return hipErrorInvalidValue;
+  }
 }
 
 // r of a product `x` (see above)
@@ -102,6 +120,42 @@ template <int SC>
 __device__ __forceinline__ float score_bound(float c, float qn, float kn, float cap2) {
   const float b = fabsf(c) * qn * kn * 1.001f;  // (the norms' own roundings)
   return (SC & kScoreCap) && b < INFINITY ? fminf(b, cap2) : b;
+}
+
+// Windowed views (kWindow). A query tile's key tiles are those of key_tiles; of a source's
+// keys (indices ascend with positions) a row sees those from the first in its window up
+// to itself or its receive limit, and those before `sink`. In the query-major kernels a
+// lane has a row: its windows' starts are in LDS (a word per source and lane of 32, read
+// on tiles that are masked), the tile's own bounds in scalar registers.
+struct WindowTiles {
+  KeyTiles recv, local;
+  int sink_r, sink_l;    // ends of the sinks
+  int last_r, last_l;    // the last row's windows begin here
+};
+__device__ __forceinline__ WindowTiles window_tiles(const int32_t* win, int q0, int q1, int r0, int r1, int l0,
+                                                    int l1) {
+  const int32_t* const a = win + 4 * size_t(q0);
+  const int32_t* const b = win + 4 * size_t(q1 - 1);
+  return {key_tiles(r0, r1, a[1], a[3]), key_tiles(l0, l1, a[0], a[2]), a[3], a[2], b[1], b[0]};
+}
+// Bytes of LDS for the rows' windows, and a lane's place there (`pair`: wave * 32 + row).
+constexpr uint32_t kWindowLds = 128 * 8;
+__device__ __forceinline__ void put_window(char* lds, int pair, const int32_t* win, int row) {
+  *reinterpret_cast<uint2*>(lds + 8 * pair) =
+      make_uint2(uint32_t(win[4 * size_t(row)]), uint32_t(win[4 * size_t(row) + 1]));
+}
+
+// A lane's 32 scores of a key tile (key k0 + 4 (lane / 32) + 8 (n / 4) + n % 4 for score n)
+// as bits: those of keys before the t-th from k0 + 4 (lane / 32) on.
+__device__ __forceinline__ uint32_t keys_below(int t) {
+  t = min(max(t, 0), 64);
+  const int n = 4 * (t >> 3) + min(t & 7, 4);
+  return n ? 0xffffffffu >> (32 - n) : 0u;
+}
+// The scores that a row sees: before `rel`, and from `from` on or before `sink`. One
+// register for all of a tile (three compared per score cost spills).
+__device__ __forceinline__ uint32_t seen_keys(int rel, int from, int sink) {
+  return keys_below(rel) & (~keys_below(from) | keys_below(sink));
 }
 
 // KV head of workgroup b, and its index among those of the head; `per` of them.

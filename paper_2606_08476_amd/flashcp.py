@@ -33,6 +33,7 @@ EXPORTS = [
     "fc_attn_fwd_partial", "fc_attn_fwd_partials", "fc_lse_merge", "fc_attn_bwd", "fc_bwd_preprocess",
     "fc_attn_bwd_pass", "fc_attn_bwd_dkdv", "fc_attn_bwd_dq", "fc_attn_bwd_noalloc", "fc_last_error",
     "fc_rope_freqs", "fc_rope_fwd", "fc_kv_gather_rope", "fc_rope_bwd",
+    "fc_view_create_windowed", "fc_view_get_window", "fc_view_export_window",
     "fc_norm_rope_fwd", "fc_kv_gather_norm_rope", "fc_norm_rope_workspace", "fc_norm_rope_bwd",
 ]
 
@@ -60,6 +61,10 @@ class TileCfg(C.Structure):
 
 class Score(C.Structure):
     _fields_ = [("cap", C.c_float), ("slopes", C.c_void_p)]
+
+
+class Window(C.Structure):
+    _fields_ = [("window", C.c_int32), ("sinks", C.c_int32)]
 
 
 class RopeCfg(C.Structure):
@@ -109,6 +114,11 @@ def _signatures():
         "fc_view_create_scored": [I32P, C.c_int32, C.POINTER(Shard), C.c_int64, C.c_int32, C.c_int32,
                                   C.c_int32, C.c_int32, C.c_int32, C.POINTER(TileCfg),
                                   C.POINTER(Score), C.POINTER(P)],
+        "fc_view_create_windowed": [I32P, C.c_int32, C.POINTER(Shard), C.c_int64, C.c_int32, C.c_int32,
+                                    C.c_int32, C.c_int32, C.c_int32, C.POINTER(TileCfg),
+                                    C.POINTER(Score), C.POINTER(Window), C.POINTER(P)],
+        "fc_view_get_window": [P, I32P, I32P],
+        "fc_view_export_window": [P, I32P, I32P, I32P],
         "fc_view_get_score": [P, C.POINTER(C.c_float), I32P, C.POINTER(C.c_float)],
         "fc_view_get_info": [P, C.POINTER(ViewInfo)],
         "fc_view_export": [P] + [I32P] * 11,
@@ -276,15 +286,17 @@ class View:
     ``tiles``: (bm_fwd, bn_fwd, bm_bwd, bn_bwd), 0 for a default; None for
     all defaults. ``cap``, ``slopes`` (hq values): the score function of every
     forward and backward call made with the view (fc_score), scores capped by cap *
-    tanh(x / cap) and less slopes[h] * distance; 0 and None for none."""
+    tanh(x / cap) and less slopes[h] * distance; 0 and None for none. ``window``,
+    ``sinks``: a query sees the last ``window`` tokens of its document up to itself and
+    the document's first ``sinks`` (fc_window); 0 for every earlier token."""
 
     def __init__(self, cu, plan, cp: int, rank: int, hq: int, hkv: int, d: int, tiles=None,
-                 cap: float = 0.0, slopes=None):
+                 cap: float = 0.0, slopes=None, window: int = 0, sinks: int = 0):
         a, p, n = _cu(cu)
         s, sp, m = _shards(plan)
         h = P()
         t = C.byref(TileCfg(*[int(x) for x in tiles])) if tiles is not None else None
-        if cap or slopes is not None:
+        if cap or slopes is not None or window or sinks:
             f = None
             if slopes is not None:
                 f = np.ascontiguousarray(slopes, dtype=np.float32)
@@ -292,8 +304,8 @@ class View:
                     raise ValueError(f"slopes has shape {f.shape}, expected ({hq},)")
                 f = f if f.flags.aligned else f.copy()
             score = Score(float(cap), None if f is None else f.ctypes.data)
-            _check(_addr().fc_view_create_scored(p, n, sp, m, cp, rank, hq, hkv, d, t, C.byref(score),
-                                                 C.byref(h)))
+            _check(_addr().fc_view_create_windowed(p, n, sp, m, cp, rank, hq, hkv, d, t, C.byref(score),
+                                                   C.byref(Window(int(window), int(sinks))), C.byref(h)))
         else:
             _check(_addr().fc_view_create(p, n, sp, m, cp, rank, hq, hkv, d, t, C.byref(h)))
         self._h = h
@@ -321,6 +333,27 @@ class View:
         _check(lib().fc_view_get_score(self.handle, C.byref(cap), C.byref(biased),
                                        f.ctypes.data_as(C.POINTER(C.c_float))))
         return cap.value, (f if biased.value else None)
+
+    @property
+    def window(self):
+        """(window, sinks), 0 for none."""
+        w, k = C.c_int32(0), C.c_int32(0)
+        _check(lib().fc_view_get_window(self.handle, C.byref(w), C.byref(k)))
+        return w.value, k.value
+
+    def export_window(self):
+        """The window tables (fc_view_export_window): ``win`` [t_q, 4] and ``wave_end``
+        [n_bwd_launch, waves, 2]; None without."""
+        on = C.c_int32(0)
+        _check(lib().fc_view_export_window(self.handle, C.byref(on), None, None))
+        if not on.value:
+            return None
+        i = self.info
+        win = np.zeros((i["t_q"], 4), dtype=np.int32)
+        end = np.zeros((i["n_bwd_launch"], i["bn_bwd"] // 32, 2), dtype=np.int32)
+        _check(lib().fc_view_export_window(self.handle, C.byref(on), win.ctypes.data_as(I32P),
+                                           end.ctypes.data_as(I32P)))
+        return dict(win=win, wave_end=end)
 
     @property
     def handle(self):
