@@ -443,8 +443,8 @@ typedef struct {
 } fc_norm;
 #define FC_NORM_EPS_MIN 5.421010862427522e-20f /* 2^-64 */
 
-/* fc_rope_fwd with q and k normalised first (q_norm, k_norm NULL: not that one; rope
- * NULL: not rotated). One launch. No output may overlap the weights. */
+/* fc_rope_fwd with q and k normalised first (q_norm, k_norm NULL: not that one, both: as
+ * fc_rope_fwd; rope NULL: not rotated). One launch. No output may overlap the weights. */
 int fc_norm_rope_fwd(fc_view view, const fc_rope* rope, const fc_norm* q_norm, const fc_norm* k_norm,
                      const fc_rows* q, const fc_rows* k, const fc_rows* v, void* stream);
 

@@ -295,6 +295,7 @@ extern "C" {
 
 int fc_norm_rope_fwd(fc_view view, const fc_rope* rope, const fc_norm* q_norm, const fc_norm* k_norm,
                      const fc_rows* q, const fc_rows* k, const fc_rows* v, void* stream) {
+  if (!q_norm && !k_norm) return fc_rope_fwd(view, rope, q, k, v, stream);
   fc::clear_error();
   const View* w;
   if (int rc = bound(view, w)) return rc;
@@ -308,6 +309,8 @@ int fc_norm_rope_fwd(fc_view view, const fc_rope* rope, const fc_norm* q_norm, c
 int fc_kv_gather_norm_rope(fc_view view, const fc_rope* rope, const fc_norm* k_norm, const void* k_packed,
                            const void* v_packed, int64_t t_packed, void* k_loc, void* v_loc, void* k_recv,
                            void* v_recv, void* stream) {
+  if (!k_norm)
+    return fc_kv_gather_rope(view, rope, k_packed, v_packed, t_packed, k_loc, v_loc, k_recv, v_recv, stream);
   fc::clear_error();
   const View* w;
   if (int rc = bound(view, w)) return rc;
@@ -362,6 +365,8 @@ int fc_norm_rope_bwd(fc_view view, const fc_rope* rope, const fc_norm* q_norm, c
                      const fc_rows* dk_recv, const fc_rows* dv_recv, const fc_norm_rows* q_in,
                      const fc_norm_rows* k_in, const fc_norm_rows* k_recv_in, void* dw_q, void* dw_k, void* ws,
                      size_t ws_bytes, void* stream) {
+  if (!q_norm && !k_norm && !dw_q && !dw_k)
+    return fc_rope_bwd(view, rope, out_bf16, dq, dk_loc, dv_loc, dk_recv, dv_recv, stream);
   fc::clear_error();
   const View* w;
   if (int rc = bound(view, w)) return rc;

@@ -69,6 +69,7 @@ struct Unit {
   }
   // the pair that values j of a (and b) are turned by, and whether they are at all
   __device__ __forceinline__ void turn(float (&a)[V], float (&b)[V], const float* c, const float* s) const {
+#pragma clang fp contract(off)
     if (!half) return;
     if constexpr (LAYOUT == kRopeNeighbours) {
 #pragma unroll
@@ -189,16 +190,54 @@ __device__ __forceinline__ void load_weights(float (&wa)[V], float (&wb)[V], con
   for (int j = 0; j < V; ++j) wa[j] = wb[j] = 1.f;
   if (!s.norm || !on) return;
   const int64_t at = int64_t(head) * s.w_stride;
+  // (one branch around all loads of a kind: a branch around each would wait for each)
+  auto load = [&](auto f32) {
+    constexpr bool F32 = decltype(f32)::value;
+#pragma unroll
+    for (int j = 0; j < V; ++j) {
+      wa[j] = load1<F32>(s.weight, at + un.at_a(j));
+      wb[j] = load1<F32>(s.weight, at + un.at_b(j));
+    }
+  };
+  if (!s.weight) return;
+  if (s.w_bf16)
+    load(std::false_type());
+  else
+    load(std::true_type());
 #pragma unroll
   for (int j = 0; j < V; ++j) {
-    const int64_t ea = at + un.at_a(j), eb = at + un.at_b(j);
-    if (s.weight) {
-      wa[j] = s.w_bf16 ? load1<false>(s.weight, ea) : load1<true>(s.weight, ea);
-      wb[j] = s.w_bf16 ? load1<false>(s.weight, eb) : load1<true>(s.weight, eb);
-    }
     wa[j] += s.offset;
     wb[j] += s.offset;
   }
+}
+
+// Sine and cosine of a turn's 64-bit fraction, within 0.72 steps: the nearest quarter turns off, |x| <= pi / 4 in two parts x + e, and
+//   sin = x + (e - x^3/6 + x^5/120 - ..),  cos = 1 - x^2/2 + (x^4/24 - .. - x e),
+// Taylor's series to x^9 and x^10 (what is left out is under 2^-28), the last sums of a large
+// and a small part. (sincospif of the fraction as fp32 is off by up to 2 steps: with it
+// 1.5 times as many of the bf16 results are not the nearest.)
+__device__ __forceinline__ void turn_sincos(uint64_t turn, float& sn, float& cs) {
+#pragma clang fp contract(off)
+  const uint32_t top = uint32_t(turn >> 32), quarter = (top + 0x20000000u) >> 30;
+  const int32_t h = int32_t(top - (quarter << 30));  // 2^-32 turns, -2^29 .. 2^29
+  constexpr float k = 0x1.921fb6p-30f, kl = -0x1.777a5cp-55f;  // 2 pi 2^-32 in two parts
+  const float f = float(h), fl = float(h - int32_t(f));
+  const float x = f * k;
+  const float e = __builtin_fmaf(f, k, -x) + __builtin_fmaf(f, kl, fl * k);
+  const float z = x * x, zl = __builtin_fmaf(x, x, -z);
+  float p = __builtin_fmaf(z, 0x1.71de3ap-19f, -0x1.a01a02p-13f);  // 1/9!, -1/7!
+  p = __builtin_fmaf(z, p, 0x1.111112p-7f);                        // 1/5!
+  p = __builtin_fmaf(z, p, -0x1.555556p-3f);                       // -1/3!
+  const float s0 = x + __builtin_fmaf(x * z, p, __builtin_fmaf(-0.5f * z, e, e));
+  float q = __builtin_fmaf(z, -0x1.27e4fcp-22f, 0x1.a01a02p-16f);  // -1/10!, 1/8!
+  q = __builtin_fmaf(z, q, -0x1.6c16c2p-10f);                      // -1/6!
+  q = __builtin_fmaf(z, q, 0x1.555556p-5f);                        // 1/4!
+  const float t = 1.f - 0.5f * z, tl = (1.f - t) - 0.5f * z;
+  const float c0 = t + __builtin_fmaf(z * z, q, tl - __builtin_fmaf(x, e, 0.5f * zl));
+  const bool swap = quarter & 1;
+  const float a = swap ? c0 : s0, b = swap ? s0 : c0;
+  sn = quarter & 2 ? -a : a;
+  cs = (quarter + 1) & 2 ? -b : b;
 }
 
 // Which tensor, rows and heads a workgroup takes.
@@ -236,7 +275,7 @@ __device__ __forceinline__ void fill_turns(const NormParams& p, const NormRows& 
     float c = 1.f, sn = 0.f;
     if (j < p.pairs) {
       const uint64_t turn = p.turn[j] * uint64_t(uint32_t(pos[i / (D / 2)]));
-      sincospif(float(int32_t(turn >> 32)) * 0x1p-31f, &sn, &c);
+      turn_sincos(turn, sn, c);
       c *= p.amplitude;
       sn *= p.amplitude * p.sign;
     }
@@ -249,6 +288,7 @@ __device__ __forceinline__ void fill_turns(const NormParams& p, const NormRows& 
 template <int D, int LAYOUT>
 __global__ __launch_bounds__(256) void norm_fwd_kernel(NormParams p) {
   constexpr int V = 8, U = norm_lanes(D, false);
+  typedef uint32_t word __attribute__((ext_vector_type(4)));
   __shared__ __attribute__((aligned(16))) float cs[2][kNormRows * D / 2];
   __shared__ int32_t pos[kNormRows];
   const Share sh = share_of(p);
@@ -257,6 +297,23 @@ __global__ __launch_bounds__(256) void norm_fwd_kernel(NormParams p) {
   const int row = slot / s.group_heads, head = sh.head0 + slot % s.group_heads;
   const bool on = row < s.step_rows && head < s.heads;
   const Unit<D, LAYOUT, V> un(threadIdx.x % U, s.rotate, p.pairs);
+  // where this thread's pieces of row r are (a thread without one: of the first row)
+  auto at = [&](int r) {
+    const bool have = on && r < sh.r1;
+    const int rr = have ? r : sh.r0;
+    const int64_t src = s.in_gather ? s.in_gather[rr] : rr;
+    return src * s.in_stride + (have ? head : 0) * D;
+  };
+  // a row's pieces are read a step ahead, the first before the sines
+  const u16* const base = static_cast<const u16*>(s.in);
+  word na = {}, nb = {};
+  auto ahead = [&](int r) {
+    if (un.odd()) return;
+    const int64_t e = at(r);
+    na = *reinterpret_cast<const word*>(base + e + un.ea);
+    nb = *reinterpret_cast<const word*>(base + e + un.eb);
+  };
+  ahead(sh.r0 + row);
   float wa[V], wb[V];
   load_weights(wa, wb, s, un, head, on);
   const int chunk = kNormRows / s.step_rows * s.step_rows;
@@ -266,10 +323,19 @@ __global__ __launch_bounds__(256) void norm_fwd_kernel(NormParams p) {
     for (int q = c0; q < c1; q += s.step_rows) {
       const int r = q + row;
       const bool have = on && r < c1;
-      const int rr = have ? r : c0;
-      const int64_t src = s.in_gather ? s.in_gather[rr] : rr;
-      const int64_t in = src * s.in_stride + (have ? head : 0) * D;
-      auto read = [&](float (&a)[V], float (&b)[V]) { load_unit<D, LAYOUT, V, false>(a, b, un, s.in, in); };
+      const word xa = na, xb = nb;
+      auto read = [&](float (&a)[V], float (&b)[V]) {
+        if (un.odd()) {
+          load_unit<D, LAYOUT, V, false>(a, b, un, s.in, at(r));
+          return;
+        }
+#pragma unroll
+        for (int j = 0; j < V; ++j) {
+          a[j] = __uint_as_float(j & 1 ? xa[j / 2] & 0xffff0000u : xa[j / 2] << 16);
+          b[j] = __uint_as_float(j & 1 ? xb[j / 2] & 0xffff0000u : xb[j / 2] << 16);
+        }
+      };
+      if (q + s.step_rows < sh.r1) ahead(r + s.step_rows);
       float a[V], b[V];
       read(a, b);
       if (s.norm) {
@@ -290,6 +356,7 @@ __global__ __launch_bounds__(256) void norm_fwd_kernel(NormParams p) {
 template <int D, int LAYOUT, bool OUT32>
 __global__ __launch_bounds__(256) void norm_bwd_kernel(NormParams p) {
   constexpr int V = 4, U = norm_lanes(D, true);
+  typedef uint32_t word2 __attribute__((ext_vector_type(2)));
   __shared__ __attribute__((aligned(16))) float cs[2][kNormRows * D / 2];
   __shared__ __attribute__((aligned(16))) float dws[256 * 2 * V];
   __shared__ int32_t pos[kNormRows];
@@ -299,6 +366,30 @@ __global__ __launch_bounds__(256) void norm_bwd_kernel(NormParams p) {
   const int row = slot / s.group_heads, head = sh.head0 + slot % s.group_heads;
   const bool on = row < s.step_rows && head < s.heads;
   const Unit<D, LAYOUT, V> un(threadIdx.x % U, s.rotate, p.pairs);
+  // where this thread's pieces of row r are (a thread without one: of the first row)
+  auto in_at = [&](int r) {
+    const bool have = on && r < sh.r1;
+    return (have ? r : sh.r0) * s.in_stride + (have ? head : 0) * D;
+  };
+  auto x_at = [&](int r) {
+    const bool have = on && r < sh.r1;
+    const int rr = have ? r : sh.r0;
+    return (s.x_gather ? s.x_gather[rr] : rr) * s.x_stride + (have ? head : 0) * D;
+  };
+  // a row's pieces are read a step ahead, the first before the sines
+  f32x4 ga = {}, gb = {};
+  word2 ya = {}, yb = {};
+  auto ahead = [&](int r) {
+    if (un.odd()) return;
+    const float* const g = static_cast<const float*>(s.in) + in_at(r);
+    ga = *reinterpret_cast<const f32x4*>(g + un.ea);
+    gb = *reinterpret_cast<const f32x4*>(g + un.eb);
+    if (!s.norm) return;
+    const u16* const x = static_cast<const u16*>(s.x) + x_at(r);
+    ya = *reinterpret_cast<const word2*>(x + un.ea);
+    yb = *reinterpret_cast<const word2*>(x + un.eb);
+  };
+  ahead(sh.r0 + row);
   float wa[V], wb[V], da[V], db[V];
   load_weights(wa, wb, s, un, head, on);
 #pragma unroll
@@ -310,18 +401,34 @@ __global__ __launch_bounds__(256) void norm_bwd_kernel(NormParams p) {
     for (int q = c0; q < c1; q += s.step_rows) {
       const int r = q + row;
       const bool have = on && r < c1;
-      const int rr = have ? r : c0, hh = have ? head : 0;
+      const int rr = have ? r : c0;
       float a[V], b[V];
-      load_unit<D, LAYOUT, V, true>(a, b, un, s.in, int64_t(rr) * s.in_stride + hh * D);
-      if (!s.norm) {
-        if (!have) continue;
-        un.turn(a, b, cs[0] + (rr - c0) * (D / 2), cs[1] + (rr - c0) * (D / 2));
+      if (un.odd()) {
+        load_unit<D, LAYOUT, V, true>(a, b, un, s.in, in_at(r));
       } else {
-        const int64_t xr = s.x_gather ? s.x_gather[rr] : rr, x = xr * s.x_stride + hh * D;
-        auto read = [&](float (&ya)[V], float (&yb)[V]) { load_unit<D, LAYOUT, V, false>(ya, yb, un, s.x, x); };
+#pragma unroll
+        for (int j = 0; j < V; ++j) {
+          a[j] = ga[j];
+          b[j] = gb[j];
+        }
+      }
+      const word2 xa = ya, xb = yb;
+      if (q + s.step_rows < sh.r1) ahead(r + s.step_rows);
+      un.turn(a, b, cs[0] + (rr - c0) * (D / 2), cs[1] + (rr - c0) * (D / 2));
+      if (s.norm) {
+        auto read = [&](float (&na)[V], float (&nb)[V]) {
+          if (un.odd()) {
+            load_unit<D, LAYOUT, V, false>(na, nb, un, s.x, x_at(r));
+            return;
+          }
+#pragma unroll
+          for (int j = 0; j < V; ++j) {
+            na[j] = __uint_as_float(j & 1 ? xa[j / 2] & 0xffff0000u : xa[j / 2] << 16);
+            nb[j] = __uint_as_float(j & 1 ? xb[j / 2] & 0xffff0000u : xb[j / 2] << 16);
+          }
+        };
         float na[V], nb[V];
         read(na, nb);
-        un.turn(a, b, cs[0] + (rr - c0) * (D / 2), cs[1] + (rr - c0) * (D / 2));
         const float sc = normalise<D, U>(na, nb, s.centred, s.eps, read);
         float m = 0.f, mn = 0.f;
 #pragma unroll
@@ -342,9 +449,8 @@ __global__ __launch_bounds__(256) void norm_bwd_kernel(NormParams p) {
           a[j] = (__builtin_fmaf(-mn, na[j], a[j]) - m) * sc;
           b[j] = (__builtin_fmaf(-mn, nb[j], b[j]) - m) * sc;
         }
-        if (!have) continue;
       }
-      store_unit<D, LAYOUT, V, OUT32>(a, b, un, s.out, int64_t(r) * s.out_stride + head * D);
+      if (have) store_unit<D, LAYOUT, V, OUT32>(a, b, un, s.out, int64_t(r) * s.out_stride + head * D);
     }
   }
   if (!s.part) return;
@@ -373,28 +479,43 @@ __global__ __launch_bounds__(256) void norm_bwd_kernel(NormParams p) {
   }
 }
 
-// 32 values per workgroup, a 32nd of the rows per thread, summed in 64 bits.
+// 32 values per workgroup, four and a 128th of the rows per thread, summed in 64 bits:
+// bound by the latency of reading what other XCDs have written, so all of a thread's rows
+// (up to 16) are read at once.
 __global__ __launch_bounds__(1024) void norm_sum_kernel(NormSum x, NormSum y) {
-  __shared__ double t[32][33];
+  __shared__ double t[128][33];
   int blk = blockIdx.x;
   const int nx = x.width / 32;
   const NormSum s = blk < nx ? x : y;
   if (blk >= nx) blk -= nx;
-  const int i = threadIdx.x & 31, k = threadIdx.x >> 5;
-  double sum = 0;
-  for (int r = k; r < s.n; r += 32) sum += double(s.part[int64_t(r) * s.width + 32 * blk + i]);
-  t[k][i] = sum;
+  const int i = 4 * (threadIdx.x & 7), k = threadIdx.x >> 3;
+  double sum[4] = {0, 0, 0, 0};
+  const float* const at = s.part + 32 * blk + i;
+  for (int r = k; r < s.n; r += 16 * 128) {
+    f32x4 v[16];
+#pragma unroll
+    for (int u = 0; u < 16; ++u)
+      if (r + 128 * u < s.n) v[u] = *reinterpret_cast<const f32x4*>(at + int64_t(r + 128 * u) * s.width);
+#pragma unroll
+    for (int u = 0; u < 16; ++u)
+      if (r + 128 * u < s.n) {
+#pragma unroll
+        for (int j = 0; j < 4; ++j) sum[j] += double(v[u][j]);
+      }
+  }
+#pragma unroll
+  for (int j = 0; j < 4; ++j) t[k][i + j] = sum[j];
   __syncthreads();
-  for (int w = 16; w; w /= 2) {
-    if (k < w) t[k][i] += t[k + w][i];
+  for (int w = 64; w; w /= 2) {
+    for (int e = threadIdx.x; e < 32 * w; e += 1024) t[e / 32][e % 32] += t[e / 32 + w][e % 32];
     __syncthreads();
   }
-  if (k == 0) {
-    const float v = float(t[0][i]);
+  if (threadIdx.x < 32) {
+    const float v = float(t[0][threadIdx.x]);
     if (s.bf16)
-      static_cast<u16*>(s.dw)[32 * blk + i] = f2bf(v);
+      static_cast<u16*>(s.dw)[32 * blk + threadIdx.x] = f2bf(v);
     else
-      static_cast<float*>(s.dw)[32 * blk + i] = v;
+      static_cast<float*>(s.dw)[32 * blk + threadIdx.x] = v;
   }
 }
 
