@@ -48,9 +48,11 @@ int64_t width_of(const View& v, const fc_norm& n, int32_t heads) {
   return n.per_head ? int64_t(heads) * v.d : v.d;
 }
 
-// How workgroups share a tensor's rows. Forward: four steps each, fewer where the
-// whole call would leave most of the card without work. Backward: sixteen at most (a
-// workgroup leaves a row of partial weight gradients).
+// How workgroups share a tensor's rows: kNormSteps steps each, fewer where the whole call
+// would leave most of the card without work. (A backward's workgroup leaves a row of
+// partial weight gradients. Of 16, 8 and 4 steps: gradients of 64K tokens over 8 ranks,
+// 32/8 heads of 128, 208, 203 and 205 us; of 50K over 4, 16/8 heads of 64, weights per
+// head, fp32, 109, 101 and 98.)
 int64_t share(fck::NormRows& k, int32_t d, bool back, int32_t steps) {
   const int32_t slots = 256 / fck::norm_lanes(d, back);
   k.head_groups = (k.heads + slots - 1) / slots;
@@ -63,7 +65,7 @@ int64_t share(fck::NormRows& k, int32_t d, bool back, int32_t steps) {
   return blocks * k.head_groups;
 }
 void share_all(fck::NormParams& p, int32_t d, bool back) {
-  for (int32_t steps = back ? 16 : 4;; steps /= 2) {
+  for (int32_t steps = fck::kNormSteps;; steps /= 2) {
     int64_t total = 0;
     for (int i = 0; i < p.n_sets; ++i) total += share(p.set[i], d, back, steps);
     if (total >= 1024 || steps == 1) return;

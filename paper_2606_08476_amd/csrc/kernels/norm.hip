@@ -85,13 +85,15 @@ struct Unit {
     } else {
       // (what is not rotated is not multiplied either: 0 times an infinity beside it)
       const int i0 = LAYOUT == kRopeHalves ? ea : V * u;
+      if (LAYOUT == kRopeHalves && !pairs) return;
 #pragma unroll
       for (int j = 0; j < V; ++j) {
-        const bool on = LAYOUT == kRopeHalves ? pairs : i0 + j < half;
+        const bool on = LAYOUT == kRopeHalves || i0 + j < half;
         const int i = on ? i0 + j : 0;
         const float x = a[j], y = b[j], cc = c[i], ss = s[i];
-        a[j] = on ? x * cc - y * ss : x;
-        b[j] = on ? y * cc + x * ss : y;
+        const float xt = x * cc - y * ss, yt = y * cc + x * ss;
+        a[j] = on ? xt : x;
+        b[j] = on ? yt : y;
       }
     }
   }
@@ -290,7 +292,7 @@ __global__ __launch_bounds__(256) void norm_fwd_kernel(NormParams p) {
   constexpr int V = 8, U = norm_lanes(D, false);
   typedef uint32_t word __attribute__((ext_vector_type(4)));
   __shared__ __attribute__((aligned(16))) float cs[2][kNormRows * D / 2];
-  __shared__ int32_t pos[kNormRows];
+  __shared__ int32_t pos[kNormRows], src[kNormBlock];
   const Share sh = share_of(p);
   const NormRows& s = sh.s;
   const int slot = threadIdx.x / U;
@@ -298,24 +300,26 @@ __global__ __launch_bounds__(256) void norm_fwd_kernel(NormParams p) {
   const bool on = row < s.step_rows && head < s.heads;
   const Unit<D, LAYOUT, V> un(threadIdx.x % U, s.rotate, p.pairs);
   // where this thread's pieces of row r are (a thread without one: of the first row)
-  auto at = [&](int r) {
+  auto at = [&](int r, const auto& source) {
     const bool have = on && r < sh.r1;
-    const int rr = have ? r : sh.r0;
-    const int64_t src = s.in_gather ? s.in_gather[rr] : rr;
-    return src * s.in_stride + (have ? head : 0) * D;
+    return source(have ? r : sh.r0) * s.in_stride + (have ? head : 0) * D;
   };
+  auto listed = [&](int r) { return int64_t(s.in_gather ? s.in_gather[r] : r); };
+  auto known = [&](int r) { return int64_t(src[r - sh.r0]); };
+  if (int(threadIdx.x) < sh.r1 - sh.r0) src[threadIdx.x] = int32_t(listed(sh.r0 + int(threadIdx.x)));
   // a row's pieces are read a step ahead, the first before the sines
   const u16* const base = static_cast<const u16*>(s.in);
   word na = {}, nb = {};
-  auto ahead = [&](int r) {
+  auto ahead = [&](int r, const auto& source) {
     if (un.odd()) return;
-    const int64_t e = at(r);
+    const int64_t e = at(r, source);
     na = *reinterpret_cast<const word*>(base + e + un.ea);
     nb = *reinterpret_cast<const word*>(base + e + un.eb);
   };
-  ahead(sh.r0 + row);
+  ahead(sh.r0 + row, listed);
   float wa[V], wb[V];
   load_weights(wa, wb, s, un, head, on);
+  __syncthreads();
   const int chunk = kNormRows / s.step_rows * s.step_rows;
   for (int c0 = sh.r0; c0 < sh.r1; c0 += chunk) {
     const int c1 = min(c0 + chunk, sh.r1);
@@ -326,7 +330,7 @@ __global__ __launch_bounds__(256) void norm_fwd_kernel(NormParams p) {
       const word xa = na, xb = nb;
       auto read = [&](float (&a)[V], float (&b)[V]) {
         if (un.odd()) {
-          load_unit<D, LAYOUT, V, false>(a, b, un, s.in, at(r));
+          load_unit<D, LAYOUT, V, false>(a, b, un, s.in, at(r, known));
           return;
         }
 #pragma unroll
@@ -335,7 +339,7 @@ __global__ __launch_bounds__(256) void norm_fwd_kernel(NormParams p) {
           b[j] = __uint_as_float(j & 1 ? xb[j / 2] & 0xffff0000u : xb[j / 2] << 16);
         }
       };
-      if (q + s.step_rows < sh.r1) ahead(r + s.step_rows);
+      if (q + s.step_rows < sh.r1) ahead(r + s.step_rows, known);
       float a[V], b[V];
       read(a, b);
       if (s.norm) {
@@ -359,7 +363,7 @@ __global__ __launch_bounds__(256) void norm_bwd_kernel(NormParams p) {
   typedef uint32_t word2 __attribute__((ext_vector_type(2)));
   __shared__ __attribute__((aligned(16))) float cs[2][kNormRows * D / 2];
   __shared__ __attribute__((aligned(16))) float dws[256 * 2 * V];
-  __shared__ int32_t pos[kNormRows];
+  __shared__ int32_t pos[kNormRows], src[kNormBlock];
   const Share sh = share_of(p);
   const NormRows& s = sh.s;
   const int slot = threadIdx.x / U;
@@ -371,27 +375,30 @@ __global__ __launch_bounds__(256) void norm_bwd_kernel(NormParams p) {
     const bool have = on && r < sh.r1;
     return (have ? r : sh.r0) * s.in_stride + (have ? head : 0) * D;
   };
-  auto x_at = [&](int r) {
+  auto x_at = [&](int r, const auto& source) {
     const bool have = on && r < sh.r1;
-    const int rr = have ? r : sh.r0;
-    return (s.x_gather ? s.x_gather[rr] : rr) * s.x_stride + (have ? head : 0) * D;
+    return source(have ? r : sh.r0) * s.x_stride + (have ? head : 0) * D;
   };
+  auto listed = [&](int r) { return int64_t(s.x_gather ? s.x_gather[r] : r); };
+  auto known = [&](int r) { return int64_t(src[r - sh.r0]); };
+  if (int(threadIdx.x) < sh.r1 - sh.r0) src[threadIdx.x] = int32_t(listed(sh.r0 + int(threadIdx.x)));
   // a row's pieces are read a step ahead, the first before the sines
   f32x4 ga = {}, gb = {};
   word2 ya = {}, yb = {};
-  auto ahead = [&](int r) {
+  auto ahead = [&](int r, const auto& source) {
     if (un.odd()) return;
     const float* const g = static_cast<const float*>(s.in) + in_at(r);
     ga = *reinterpret_cast<const f32x4*>(g + un.ea);
     gb = *reinterpret_cast<const f32x4*>(g + un.eb);
     if (!s.norm) return;
-    const u16* const x = static_cast<const u16*>(s.x) + x_at(r);
+    const u16* const x = static_cast<const u16*>(s.x) + x_at(r, source);
     ya = *reinterpret_cast<const word2*>(x + un.ea);
     yb = *reinterpret_cast<const word2*>(x + un.eb);
   };
-  ahead(sh.r0 + row);
+  ahead(sh.r0 + row, listed);
   float wa[V], wb[V], da[V], db[V];
   load_weights(wa, wb, s, un, head, on);
+  __syncthreads();
 #pragma unroll
   for (int j = 0; j < V; ++j) da[j] = db[j] = 0.f;
   const int chunk = kNormRows / s.step_rows * s.step_rows;
@@ -413,12 +420,12 @@ __global__ __launch_bounds__(256) void norm_bwd_kernel(NormParams p) {
         }
       }
       const word2 xa = ya, xb = yb;
-      if (q + s.step_rows < sh.r1) ahead(r + s.step_rows);
+      if (q + s.step_rows < sh.r1) ahead(r + s.step_rows, known);
       un.turn(a, b, cs[0] + (rr - c0) * (D / 2), cs[1] + (rr - c0) * (D / 2));
       if (s.norm) {
         auto read = [&](float (&na)[V], float (&nb)[V]) {
           if (un.odd()) {
-            load_unit<D, LAYOUT, V, false>(na, nb, un, s.x, x_at(r));
+            load_unit<D, LAYOUT, V, false>(na, nb, un, s.x, x_at(r, known));
             return;
           }
 #pragma unroll

@@ -37,6 +37,8 @@ struct NormRows {
 constexpr int kNormSets = 5;
 // rows whose sines and cosines are in LDS at a time
 constexpr int kNormRows = 16;
+// the most rows of a workgroup
+constexpr int kNormSteps = 4, kNormBlock = kNormSteps * kNormRows;
 // threads of a head: two pieces of 8 (forward) or 4 (backward) values each
 constexpr int norm_lanes(int d, bool back) { return d / (back ? 8 : 16); }
 

@@ -72,11 +72,6 @@ class RopeCfg(C.Structure):
                 ("amplitude", C.c_float), ("inv_freq", C.c_void_p)]
 
 
-class NormCfg(C.Structure):
-    _fields_ = [("weight", C.c_void_p), ("w_bf16", C.c_int32), ("per_head", C.c_int32),
-                ("centred", C.c_int32), ("offset", C.c_float), ("eps", C.c_float)]
-
-
 class ViewInfo(C.Structure):
     _fields_ = [
         ("t_q", C.c_int32), ("t_recv", C.c_int32), ("n_seg", C.c_int32), ("n_pieces", C.c_int32),
@@ -791,25 +786,23 @@ class HeadNorm:
         self.weight, self.eps, self.offset, self.centred = weight, float(eps), float(offset), bool(centred)
 
 
-def _norm(norm, heads, d, name, dev):
-    """fc_norm of a HeadNorm (kept alive by the caller), None for None."""
+def _norm(norm, shape, name, dev):
+    """fc_norm of a HeadNorm (as bytes) for rows of `shape`, None for None."""
     if norm is None:
         return None
     w = norm.weight
     if w is None:
-        return NormCfg(None, 0, 0, int(norm.centred), norm.offset, norm.eps)
-    if w.shape != (d,) and w.shape != (heads, d):
-        raise ValueError(f"{name} weight has shape {tuple(w.shape)}, expected {(d,)} or {(heads, d)}")
-    if not w.is_contiguous():
-        raise ValueError(f"{name} weight must be contiguous")
+        return _NORM.pack(0, 0, 0, norm.centred, norm.offset, norm.eps)
+    n = w.dim()
+    if w.shape != shape[3 - n:] or not w.is_contiguous():
+        raise ValueError(f"{name} weight must be contiguous and have shape {shape[2:]} or {shape[1:]}, "
+                         f"got {tuple(w.shape)}")
     if dev >= 0 and w.get_device() != dev:
         raise ValueError(f"{name} weight is on device {w.get_device()}, the current one is {dev}")
-    return NormCfg(w.data_ptr(), int(w.dtype is BF), int(w.dim() == 2), int(norm.centred), norm.offset,
-                   norm.eps)
+    return _NORM.pack(w.data_ptr(), w.dtype is BF, n == 2, norm.centred, norm.offset, norm.eps)
 
 
-def _ref(x):
-    return None if x is None else C.addressof(x)
+_NORM = struct.Struct("Piiiff4x")  # fc_norm
 
 
 def fc_norm_rope_fwd(view: View, rope, q_norm, k_norm, q, k, v, q_out, k_out, v_out):
@@ -818,8 +811,8 @@ def fc_norm_rope_fwd(view: View, rope, q_norm, k_norm, q, k, v, q_out, k_out, v_
     dev = _row_device(view)
     a = [_rows(q, q_out, view._q, BF, BF, "q", dev), _rows(k, k_out, view._kv, BF, BF, "k", dev),
          _rows(v, v_out, view._kv, BF, BF, "v", dev)]
-    qn, kn = _norm(q_norm, view._q[1], view._q[2], "q", dev), _norm(k_norm, view._kv[1], view._kv[2], "k", dev)
-    _check(lib().fc_norm_rope_fwd(view.handle, None if rope is None else rope._p, _ref(qn), _ref(kn), *a,
+    _check(lib().fc_norm_rope_fwd(view.handle, None if rope is None else rope._p,
+                                  _norm(q_norm, view._q, "q", dev), _norm(k_norm, view._kv, "k", dev), *a,
                                   _stream()))
 
 
@@ -832,9 +825,8 @@ def fc_kv_gather_norm_rope(view: View, rope, k_norm, k_packed, v_packed, k_loc, 
     KV, KR = view._kv, view._kvr
     T = k_packed.shape[0]
     packed = (T, KV[1], KV[2])
-    kn = _norm(k_norm, KV[1], KV[2], "k", dev)
     _check(lib().fc_kv_gather_norm_rope(
-        view.handle, None if rope is None else rope._p, _ref(kn), _ptr(k_packed, packed, BF, "k_packed"),
+        view.handle, None if rope is None else rope._p, _norm(k_norm, KV, "k", dev), _ptr(k_packed, packed, BF, "k_packed"),
         _ptr(v_packed, packed, BF, "v_packed"), T, _ptr(k_loc, KV, BF, "k_loc"),
         _ptr(v_loc, KV, BF, "v_loc"), _ptr(k_recv, KR, BF, "k_recv"), _ptr(v_recv, KR, BF, "v_recv"),
         _stream()))
@@ -843,8 +835,8 @@ def fc_kv_gather_norm_rope(view: View, rope, k_norm, k_packed, v_packed, k_loc, 
 def fc_norm_rope_workspace(view: View, q_norm, k_norm) -> int:
     """Workspace bytes of fc_norm_rope_bwd with gradients of these norms' weights."""
     n = C.c_size_t(0)
-    qn, kn = _norm(q_norm, view._q[1], view._q[2], "q", -1), _norm(k_norm, view._kv[1], view._kv[2], "k", -1)
-    _check(lib().fc_norm_rope_workspace(view.handle, _ref(qn), _ref(kn), C.byref(n)))
+    _check(lib().fc_norm_rope_workspace(view.handle, _norm(q_norm, view._q, "q", -1),
+                                        _norm(k_norm, view._kv, "k", -1), C.byref(n)))
     return n.value
 
 
@@ -863,7 +855,7 @@ def fc_norm_rope_bwd(view: View, rope, q_norm, k_norm, dq, dk_loc, dv_loc, dk_re
          _rows(dv_loc, dv_loc_out, KV, F32, dt, "dv_loc", dev),
          _rows(dk_recv, dk_recv_out, KR, F32, dt, "dk_recv", dev),
          _rows(dv_recv, dv_recv_out, KR, F32, dt, "dv_recv", dev)]
-    qn, kn = _norm(q_norm, Q[1], Q[2], "q", dev), _norm(k_norm, KV[1], KV[2], "k", dev)
+    qn, kn = _norm(q_norm, Q, "q", dev), _norm(k_norm, KV, "k", dev)
 
     def given(t, shape, name, packed):
         return None if t is None else _NORM_ROWS.pack(*_row_ptr(t, shape, BF, name, dev), packed)
@@ -883,7 +875,7 @@ def fc_norm_rope_bwd(view: View, rope, q_norm, k_norm, dq, dk_loc, dv_loc, dk_re
         dws.append(None if dw is None else dw.data_ptr())
     if ws is not None and dev >= 0 and ws.get_device() != dev:
         raise ValueError(f"ws is on device {ws.get_device()}, the current one is {dev}")
-    _check(lib().fc_norm_rope_bwd(view.handle, None if rope is None else rope._p, _ref(qn), _ref(kn),
+    _check(lib().fc_norm_rope_bwd(view.handle, None if rope is None else rope._p, qn, kn,
                                   int(dt is BF), *a, *x, *dws, *_ws(ws), _stream()))
 
 
