@@ -22,8 +22,9 @@ __global__ __launch_bounds__(256, 2) void attn_bwd_dq_scored_kernel(DqParams p) 
   dq_tile<D, HPW, D == 64 && HPW != 4, SC>(p, blockIdx.x, smem);
 }
 
+// (Windows with slopes at head dim 128 take 257 registers and more.)
 template <int D, int HPW, int KIND>
-__global__ __launch_bounds__(256, 2) void attn_bwd_dq_window_kernel(DqParams p) {
+__global__ __launch_bounds__(256, D == 128 && (KIND & kScoreBias) ? 1 : 2) void attn_bwd_dq_window_kernel(DqParams p) {
   __shared__ __attribute__((aligned(16))) char smem[DqLds<D, KIND>::bytes];
   dq_tile<D, HPW, D == 64 && HPW != 4, KIND>(p, blockIdx.x, smem);
 }

@@ -299,7 +299,30 @@ __device__ __forceinline__ void dq_tile(const DqParams& p, int b, char* smem) {
           dp[mb] = __builtin_bit_cast(f32x16, y);
         }
       };
-      auto dsv = [&](int mb, int i) { dp[mb][i] *= s[mb][i]; };
+      float pmax = 0.f;  // WIN: of the half's P (capped: times a quarter of 1 - tanh^2)
+      auto dsv = [&](int mb, int i) {
+        if (WIN) pmax = fmaxf(pmax, s[mb][i]);
+        dp[mb][i] *= s[mb][i];
+      };
+      // WIN: a short window's P are large, and dQ a difference of a few large terms: where
+      // any P of a half tile is above 1/16, the bf16 residuals of its dS go through the
+      // product too, as in dK/dV
+      auto residual = [&](int mb) {
+        if (!__any(pmax > (CAP ? 1.f / 64 : 1.f / 16))) return;
+        const bf16x8 lo[2] = {lo8(dp[mb], 0, sb[2 * mb]), lo8(dp[mb], 8, sb[2 * mb + 1])};
+        bf16x8 op[2];
+        auto rk = [&](int m) {
+          const uint32_t ro = KO + (2 * mb + m / DB) * 32 * D;
+          op[m % 2] = cat8(lds_tr(smem, pt[m % DB][0], ro), lds_tr(smem, pt[m % DB][1], ro));
+        };
+        rk(0);
+        static_for<0, 2 * DB>([&](auto mc) {
+          constexpr int m = decltype(mc)::value;
+          if (m + 1 < 2 * DB) rk(m + 1);
+          dq[m % DB] = mfma32(op[m % 2], lo[m / DB], dq[m % DB]);
+          __builtin_amdgcn_sched_barrier(0);
+        });
+      };
       rd(0);
       rd(1);
       static_for<0, NS>([&](auto nc) {
@@ -328,6 +351,10 @@ __device__ __forceinline__ void dq_tile(const DqParams& p, int b, char* smem) {
             for (int e = ks * EP; e < (ks + 1) * EP; ++e) dsv(0, e);
             if ((ks + 1) * EP == 8) sb[0] = pack8(dp[0], 0);
             if ((ks + 1) * EP == 16) sb[1] = pack8(dp[0], 8);
+            if (WIN && ks == KS - 1) {
+              residual(0);
+              pmax = 0.f;
+            }
           }
         } else {
           const int u = n - 4 * KS, kk = u / DB, db = u % DB;
@@ -338,6 +365,7 @@ __device__ __forceinline__ void dq_tile(const DqParams& p, int b, char* smem) {
             for (int e = u * EQ; e < (u + 1) * EQ; ++e) dsv(1, e);
             if ((u + 1) * EQ == 8) sb[2] = pack8(dp[1], 0);
             if ((u + 1) * EQ == 16) sb[3] = pack8(dp[1], 8);
+            if (WIN && u == 2 * DB - 1) residual(1);
           }
         }
         __builtin_amdgcn_sched_barrier(0);
