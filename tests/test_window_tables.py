@@ -215,3 +215,26 @@ def test_refusals():
     assert v.window == (4, 1) and v.score[0] == 30.0
     e = F.View([0, 10], plan, 2, 1, 4, 2, 64, window=4)   # no rows
     assert e.info["t_q"] == e.info["t_recv"] == 0 and e.export_window() is None
+
+
+def test_windowed_views_under_sanitizers(tmp_path):
+    """Every attention entry point on windowed views in a host build under AddressSanitizer
+    and UndefinedBehaviorSanitizer, with stub launchers that walk the tables."""
+    import os
+    import shutil
+    import subprocess
+    if shutil.which("g++") is None:
+        pytest.skip("needs g++")
+    root = os.path.dirname(os.path.dirname(os.path.abspath(__file__)))
+    host = os.path.join(root, "paper_2606_08476_amd", "csrc", "host")
+    exe = tmp_path / "window_driver"
+    cmd = ["g++", "-std=c++17", "-O1", "-g", "-fno-omit-frame-pointer",
+           "-fsanitize=address,undefined", "-fno-sanitize-recover=all",
+           "-D__HIP_PLATFORM_AMD__", "-I/opt/rocm/include", "-I", os.path.join(root, "include"),
+           *[os.path.join(host, f) for f in ("plan.cpp", "view.cpp", "api.cpp")],
+           os.path.join(root, "tests", "sanitize", "window_driver.cpp"), "-o", str(exe)]
+    r = subprocess.run(cmd, capture_output=True, text=True)
+    assert r.returncode == 0, r.stderr[-4000:]
+    r = subprocess.run([str(exe)], capture_output=True, text=True, timeout=300)
+    assert r.returncode == 0, (r.stdout + r.stderr)[-4000:]
+    assert "all checks passed" in r.stdout
