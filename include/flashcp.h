@@ -473,8 +473,8 @@ int fc_norm_rope_workspace(fc_view view, const fc_norm* q_norm, const fc_norm* k
  * written, not added to: sums over the tensors given, own and received keys (zeros if
  * none is given or has a row); NULL: not wanted. The sums are reproducible: no atomics.
  * ws: device, as fc_norm_rope_workspace says, if any dw is wanted. Outputs may be their
- * own gradients (in place, fp32) and overlap nothing else that is read or written. Two
- * launches. */
+ * own gradients (in place, fp32) and overlap nothing else that is read or written. One
+ * launch, two or three with dw. */
 int fc_norm_rope_bwd(fc_view view, const fc_rope* rope, const fc_norm* q_norm, const fc_norm* k_norm,
                      int32_t out_bf16, const fc_rows* dq, const fc_rows* dk_loc, const fc_rows* dv_loc,
                      const fc_rows* dk_recv, const fc_rows* dv_recv, const fc_norm_rows* q_in,

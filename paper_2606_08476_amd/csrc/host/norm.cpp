@@ -104,6 +104,12 @@ int check_stride(int64_t stride, int64_t width, int64_t size) {
   return FC_OK;
 }
 
+// Behind the partial rows, if there are many: the sums of their slices.
+int64_t slice_bytes(int64_t rows, int64_t width) {
+  const int32_t n = fck::norm_slices(rows);
+  return n > 1 ? n * width * int64_t(sizeof(double)) : 0;
+}
+
 struct Weights {  // of a backward call
   void* dw[2];
   const fc_norm* norm[2];
@@ -185,8 +191,8 @@ int run(const View& v, const fc_rope* rope, std::initializer_list<Set> sets, boo
   }
   if (!given) return fail(FC_ERR_INVALID_ARG, "no rows given");
   share_all(p, v.d, back);
-  // weights' gradients: their partial rows and they themselves
-  int64_t rows[2], bytes[2];
+  // weights' gradients: their partial rows, their slices' sums, and they themselves
+  int64_t rows[2], bytes[2], width[2] = {0, 0};
   part_sizes(p, sets, v, rows, bytes);
   Span more[3];  // dw, dw, workspace
   int n_more = 0;
@@ -195,7 +201,7 @@ int run(const View& v, const fc_rope* rope, std::initializer_list<Set> sets, boo
     int64_t need = 0;
     for (int i = 0; i < 2; ++i) {
       if (!w->dw[i]) {
-        bytes[i] = 0;
+        rows[i] = bytes[i] = 0;
         continue;
       }
       if (!w->norm[i] || !w->norm[i]->weight)
@@ -203,9 +209,10 @@ int run(const View& v, const fc_rope* rope, std::initializer_list<Set> sets, boo
       if (int rc = check_norm(w->norm[i])) return rc;
       if (reinterpret_cast<uintptr_t>(w->dw[i]) % (w->norm[i]->w_bf16 ? 2 : 4))
         return fail(FC_ERR_INVALID_ARG, "weights must be aligned to their type");
-      const int64_t n = width_of(v, *w->norm[i], heads[i]) * (w->norm[i]->w_bf16 ? 2 : 4);
+      width[i] = width_of(v, *w->norm[i], heads[i]);
+      const int64_t n = width[i] * (w->norm[i]->w_bf16 ? 2 : 4);
       more[n_more++] = {reinterpret_cast<uintptr_t>(w->dw[i]), n, n, 1};
-      need += bytes[i];
+      need += bytes[i] + slice_bytes(rows[i], width[i]);
     }
     if (need) {
       if (!w->ws || int64_t(w->ws_bytes) < need)
@@ -241,19 +248,28 @@ int run(const View& v, const fc_rope* rope, std::initializer_list<Set> sets, boo
     for (int j = 0; j < n_more; ++j)
       if (ws.touches(more[j])) return fail(FC_ERR_INVALID_ARG, "weights' gradients or workspace overlap");
   }
-  float* part[2] = {nullptr, nullptr};
+  fck::NormSum sum[2] = {};
   if (back) {
-    int64_t at[2] = {0, bytes[0] / int64_t(sizeof(float))};
-    part[0] = static_cast<float*>(w->ws);
-    part[1] = part[0] + at[1];
+    char* at = static_cast<char*>(w->ws);
+    float* part[2];
+    for (int i = 0; i < 2; ++i) {
+      part[i] = reinterpret_cast<float*>(at);
+      at += bytes[i];
+    }
+    for (int i = 0; i < 2; ++i)
+      if (w->dw[i]) {
+        sum[i] = {part[i], int32_t(rows[i]), int32_t(width[i]), w->dw[i], w->norm[i]->w_bf16 != 0,
+                  fck::norm_slices(rows[i]), reinterpret_cast<double*>(at)};
+        at += slice_bytes(rows[i], width[i]);
+      }
     int i = 0;
     for (const Set& s : sets) {
       if (!s.rows || !(s.recv ? v.t_recv() : v.t_q())) continue;
       fck::NormRows& k = p.set[i++];
       if (s.dw < 0 || !s.norm || !w->dw[s.dw]) continue;
-      k.part_width = int32_t(width_of(v, *s.norm, s.heads));
-      k.part = static_cast<float*>(w->ws) + at[s.dw];
-      at[s.dw] += part_rows(k) * k.part_width;
+      k.part_width = int32_t(width[s.dw]);
+      k.part = part[s.dw];
+      part[s.dw] += part_rows(k) * k.part_width;
     }
   }
   p.amplitude = 1.f;
@@ -271,15 +287,7 @@ int run(const View& v, const fc_rope* rope, std::initializer_list<Set> sets, boo
   }
   hipStream_t st = reinterpret_cast<hipStream_t>(stream);
   hipError_t e = back ? fck::launch_norm_bwd(p, v.d, layout, out_f32, st) : fck::launch_norm_fwd(p, v.d, layout, st);
-  if (e == hipSuccess && back) {
-    fck::NormSum sum[2] = {};
-    const int32_t heads[2] = {v.hq, v.hkv};
-    for (int i = 0; i < 2; ++i)
-      if (w->dw[i])
-        sum[i] = {part[i], int32_t(bytes[i] ? rows[i] : 0), int32_t(width_of(v, *w->norm[i], heads[i])), w->dw[i],
-                  w->norm[i]->w_bf16 != 0};
-    e = fck::launch_norm_sum(sum[0], sum[1], st);
-  }
+  if (e == hipSuccess && back) e = fck::launch_norm_sum(sum[0], sum[1], st);
   if (e != hipSuccess) return fail(FC_ERR_HIP, std::string("norm launch: ") + hipGetErrorString(e));
   return FC_OK;
 }
@@ -352,13 +360,17 @@ int fc_norm_rope_workspace(fc_view view, const fc_norm* q_norm, const fc_norm* k
   const Set each[3] = {{nullptr, v.hq, false, true, false, q_norm, nullptr, 0},
                        {nullptr, v.hkv, false, true, false, k_norm, nullptr, 1},
                        {nullptr, v.hkv, true, true, false, k_norm, nullptr, 1}};
+  int64_t rows[2] = {0, 0}, width[2] = {0, 0};
   for (const Set& s : each) {
     if (!s.norm || !(s.recv ? v.t_recv() : v.t_q())) continue;
     fck::NormParams p{};
     add_set(p, v, s);
     share_all(p, v.d, true);
-    *bytes += size_t(part_rows(p.set[0])) * size_t(width_of(v, *s.norm, s.heads)) * sizeof(float);
+    rows[s.dw] += part_rows(p.set[0]);
+    width[s.dw] = width_of(v, *s.norm, s.heads);
   }
+  for (int i = 0; i < 2; ++i)
+    *bytes += size_t(rows[i] * width[i] * int64_t(sizeof(float)) + slice_bytes(rows[i], width[i]));
   return FC_OK;
 }
 

@@ -99,30 +99,23 @@ struct Unit {
   }
 };
 
-// V bf16 values, 16 or 8 bytes.
-template <int V>
-__device__ __forceinline__ void load_bf(float (&x)[V], const void* p, int64_t e) {
-  typedef uint32_t word __attribute__((ext_vector_type(V / 2)));
-  const word w = *reinterpret_cast<const word*>(static_cast<const char*>(p) + 2 * e);
-#pragma unroll
-  for (int j = 0; j < V; ++j) x[j] = __uint_as_float(j & 1 ? w[j / 2] & 0xffff0000u : w[j / 2] << 16);
-}
-
+// A unit's values, one by one (odd halves; elsewhere a piece is a load of its own).
 template <int D, int LAYOUT, int V, bool F32>
-__device__ __forceinline__ void load_unit(float (&a)[V], float (&b)[V], const Unit<D, LAYOUT, V>& un,
-                                          const void* p, int64_t at) {
-  if (un.odd()) {
+__device__ __forceinline__ void load_odd(float (&a)[V], float (&b)[V], const Unit<D, LAYOUT, V>& un,
+                                         const void* p, int64_t at) {
 #pragma unroll
-    for (int j = 0; j < V; ++j) {
-      a[j] = load1<F32>(p, at + un.at_a(j));
-      b[j] = load1<F32>(p, at + un.at_b(j));
-    }
-  } else if constexpr (F32) {
-    Piece<true>::load(a, p, at + un.ea);
-    Piece<true>::load(b, p, at + un.eb);
-  } else {
-    load_bf(a, p, at + un.ea);
-    load_bf(b, p, at + un.eb);
+  for (int j = 0; j < V; ++j) {
+    a[j] = load1<F32>(p, at + un.at_a(j));
+    b[j] = load1<F32>(p, at + un.at_b(j));
+  }
+}
+// Two pieces of V bf16 values as they are read.
+template <int V, class W>
+__device__ __forceinline__ void unpack(float (&a)[V], float (&b)[V], const W& x, const W& y) {
+#pragma unroll
+  for (int j = 0; j < V; ++j) {
+    a[j] = __uint_as_float(j & 1 ? x[j / 2] & 0xffff0000u : x[j / 2] << 16);
+    b[j] = __uint_as_float(j & 1 ? y[j / 2] & 0xffff0000u : y[j / 2] << 16);
   }
 }
 template <int D, int LAYOUT, int V, bool F32>
@@ -329,15 +322,10 @@ __global__ __launch_bounds__(256) void norm_fwd_kernel(NormParams p) {
       const bool have = on && r < c1;
       const word xa = na, xb = nb;
       auto read = [&](float (&a)[V], float (&b)[V]) {
-        if (un.odd()) {
-          load_unit<D, LAYOUT, V, false>(a, b, un, s.in, at(r, known));
-          return;
-        }
-#pragma unroll
-        for (int j = 0; j < V; ++j) {
-          a[j] = __uint_as_float(j & 1 ? xa[j / 2] & 0xffff0000u : xa[j / 2] << 16);
-          b[j] = __uint_as_float(j & 1 ? xb[j / 2] & 0xffff0000u : xb[j / 2] << 16);
-        }
+        if (un.odd())
+          load_odd<D, LAYOUT, V, false>(a, b, un, s.in, at(r, known));
+        else
+          unpack(a, b, xa, xb);
       };
       if (q + s.step_rows < sh.r1) ahead(r + s.step_rows, known);
       float a[V], b[V];
@@ -411,7 +399,7 @@ __global__ __launch_bounds__(256) void norm_bwd_kernel(NormParams p) {
       const int rr = have ? r : c0;
       float a[V], b[V];
       if (un.odd()) {
-        load_unit<D, LAYOUT, V, true>(a, b, un, s.in, in_at(r));
+        load_odd<D, LAYOUT, V, true>(a, b, un, s.in, in_at(r));
       } else {
 #pragma unroll
         for (int j = 0; j < V; ++j) {
@@ -424,15 +412,10 @@ __global__ __launch_bounds__(256) void norm_bwd_kernel(NormParams p) {
       un.turn(a, b, cs[0] + (rr - c0) * (D / 2), cs[1] + (rr - c0) * (D / 2));
       if (s.norm) {
         auto read = [&](float (&na)[V], float (&nb)[V]) {
-          if (un.odd()) {
-            load_unit<D, LAYOUT, V, false>(na, nb, un, s.x, x_at(r, known));
-            return;
-          }
-#pragma unroll
-          for (int j = 0; j < V; ++j) {
-            na[j] = __uint_as_float(j & 1 ? xa[j / 2] & 0xffff0000u : xa[j / 2] << 16);
-            nb[j] = __uint_as_float(j & 1 ? xb[j / 2] & 0xffff0000u : xb[j / 2] << 16);
-          }
+          if (un.odd())
+            load_odd<D, LAYOUT, V, false>(na, nb, un, s.x, x_at(r, known));
+          else
+            unpack(na, nb, xa, xb);
         };
         float na[V], nb[V];
         read(na, nb);
@@ -486,44 +469,61 @@ __global__ __launch_bounds__(256) void norm_bwd_kernel(NormParams p) {
   }
 }
 
-// 32 values per workgroup, four and a 128th of the rows per thread, summed in 64 bits:
-// bound by the latency of reading what other XCDs have written, so all of a thread's rows
-// (up to 16) are read at once.
-__global__ __launch_bounds__(1024) void norm_sum_kernel(NormSum x, NormSum y) {
-  __shared__ double t[128][33];
+// kSumCols values and a slice of the rows per workgroup, added in 64 bits, rows by 16
+// threads each: partial rows to a row per slice (FINAL false), and these, or few partial
+// rows, to the gradient. Bound by the latency of reading what other XCDs wrote, twice. A
+// second launch because anything else is slower: 10751 rows of 128 values (gradients of
+// 64K tokens over 8 ranks, 32/8 heads) take 24 us in one launch of 32 values and every row
+// per workgroup, 18 of eight values, 18 with the last slice's workgroup adding them up (whose
+// fence writes back an L2 full of the gradients), and 10 in two.
+template <bool FINAL>
+__global__ __launch_bounds__(256) void norm_sum_kernel(NormSum x, NormSum y) {
+  constexpr int Q = kSumCols / 4, R = 256 / Q, N = kSumRows / R;  // threads of a row; rows at a time
+  __shared__ double t[R][kSumCols];
   int blk = blockIdx.x;
-  const int nx = x.width / 32;
+  const int nx = x.width / kSumCols * (FINAL ? 1 : x.slices);
   const NormSum s = blk < nx ? x : y;
   if (blk >= nx) blk -= nx;
-  const int i = 4 * (threadIdx.x & 7), k = threadIdx.x >> 3;
+  const int slices = FINAL ? 1 : s.slices;
+  const int col = blk / slices, slice = blk % slices, tid = threadIdx.x;
+  const int i = 4 * (tid % Q), k = tid / Q;
+  const bool sums = FINAL && s.slices > 1;  // rows are slices' sums
+  const int n = sums ? s.slices : s.n;
+  const int r0 = int(int64_t(n) * slice / slices), r1 = int(int64_t(n) * (slice + 1) / slices);
   double sum[4] = {0, 0, 0, 0};
-  const float* const at = s.part + 32 * blk + i;
-  for (int r = k; r < s.n; r += 16 * 128) {
-    f32x4 v[16];
+  auto add = [&](const auto* at, auto v) {
+    typedef decltype(v) vec;
+    for (int r = r0 + k; r < r1; r += N * R) {
+      vec x4[N];
 #pragma unroll
-    for (int u = 0; u < 16; ++u)
-      if (r + 128 * u < s.n) v[u] = *reinterpret_cast<const f32x4*>(at + int64_t(r + 128 * u) * s.width);
+      for (int u = 0; u < N; ++u)
+        if (r + R * u < r1) x4[u] = *reinterpret_cast<const vec*>(at + int64_t(r + R * u) * s.width);
 #pragma unroll
-    for (int u = 0; u < 16; ++u)
-      if (r + 128 * u < s.n) {
+      for (int u = 0; u < N; ++u)
+        if (r + R * u < r1) {
 #pragma unroll
-        for (int j = 0; j < 4; ++j) sum[j] += double(v[u][j]);
-      }
-  }
+          for (int j = 0; j < 4; ++j) sum[j] += double(x4[u][j]);
+        }
+    }
+  };
+  typedef double f64x4 __attribute__((ext_vector_type(4)));
+  if (sums)
+    add(s.rows + kSumCols * col + i, f64x4{});
+  else
+    add(s.part + kSumCols * col + i, f32x4{});
 #pragma unroll
   for (int j = 0; j < 4; ++j) t[k][i + j] = sum[j];
   __syncthreads();
-  for (int w = 64; w; w /= 2) {
-    for (int e = threadIdx.x; e < 32 * w; e += 1024) t[e / 32][e % 32] += t[e / 32 + w][e % 32];
-    __syncthreads();
-  }
-  if (threadIdx.x < 32) {
-    const float v = float(t[0][threadIdx.x]);
-    if (s.bf16)
-      static_cast<u16*>(s.dw)[32 * blk + threadIdx.x] = f2bf(v);
-    else
-      static_cast<float*>(s.dw)[32 * blk + threadIdx.x] = v;
-  }
+  if (tid >= kSumCols) return;
+  double v = 0;
+  for (int j = 0; j < R; ++j) v += t[j][tid];
+  const int at = kSumCols * col + tid;
+  if constexpr (!FINAL)
+    s.rows[int64_t(slice) * s.width + at] = v;
+  else if (s.bf16)
+    static_cast<u16*>(s.dw)[at] = f2bf(float(v));
+  else
+    static_cast<float*>(s.dw)[at] = float(v);
 }
 
 template <int D, int LAYOUT>
@@ -565,9 +565,18 @@ hipError_t launch_norm_bwd(const NormParams& p, int d, int layout, bool out_f32,
 }
 
 hipError_t launch_norm_sum(const NormSum& a, const NormSum& b, hipStream_t s) {
-  const unsigned blocks = unsigned(a.width + b.width) / 32;
+  // (those of few rows have no part in the first)
+  NormSum many[2] = {a, b};
+  for (NormSum& m : many)
+    if (m.slices <= 1) m.width = 0;
+  const int32_t first = many[0].width / kSumCols * many[0].slices + many[1].width / kSumCols * many[1].slices;
+  if (first) {
+    hipLaunchKernelGGL((norm_sum_kernel<false>), dim3(unsigned(first)), dim3(256), 0, s, many[0], many[1]);
+    if (const hipError_t e = hipGetLastError(); e != hipSuccess) return e;
+  }
+  const unsigned blocks = unsigned(a.width + b.width) / kSumCols;
   if (!blocks) return hipSuccess;
-  hipLaunchKernelGGL(norm_sum_kernel, dim3(blocks), dim3(1024), 0, s, a, b);
+  hipLaunchKernelGGL((norm_sum_kernel<true>), dim3(blocks), dim3(256), 0, s, a, b);
   return hipGetLastError();
 }
 

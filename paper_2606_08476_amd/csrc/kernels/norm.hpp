@@ -54,13 +54,21 @@ struct NormParams {
 hipError_t launch_norm_fwd(const NormParams& p, int d, int layout, hipStream_t s);
 hipError_t launch_norm_bwd(const NormParams& p, int d, int layout, bool out_f32, hipStream_t s);
 
-// Sums of partial rows: dw[e] = sum of part[r * width + e] over n rows.
+// Sums of partial rows: dw[e] = sum of part[r * width + e] over n rows; of many rows
+// (norm_slices over 1) first of `slices` of them, into a row of 64-bit sums each.
 struct NormSum {
   const float* part;
   int32_t n, width;
   void* dw;
   int32_t bf16;
+  int32_t slices;
+  double* rows;
 };
+constexpr int kSumCols = 64, kSumRows = 128, kSumSlices = 64;
+inline int32_t norm_slices(int64_t n) {
+  const int64_t s = n / kSumRows;
+  return int32_t(s < 1 ? 1 : s > kSumSlices ? kSumSlices : s);
+}
 // (one or two of them; width 0: none)
 hipError_t launch_norm_sum(const NormSum& a, const NormSum& b, hipStream_t s);
 

@@ -53,6 +53,7 @@ struct Freqs {
 
 fck::NormParams g_norm;
 fck::NormSum g_sum[2];
+int g_sliced = 0;  // sums in more than one slice
 int g_norm_layout = -1;
 bool g_back = false, g_out32 = false;
 uintptr_t g_ws = 0;
@@ -114,8 +115,20 @@ hipError_t launch_norm_sum(const NormSum& a, const NormSum& b, hipStream_t) {
   g_sum[0] = a;
   g_sum[1] = b;
   for (const NormSum& s : g_sum) {
-    CHECK(s.width % 32 == 0 && s.n >= 0);
+    CHECK(s.width % kSumCols == 0 && s.n >= 0 && (!s.width || s.slices == norm_slices(s.n)));
     if (!s.width || !s.n) continue;
+    const uintptr_t end = g_ws + g_ws_bytes;
+    CHECK(reinterpret_cast<uintptr_t>(s.part) >= g_ws);
+    if (s.slices > 1) {
+      // the slices' rows lie behind all partial rows, and not in each other's
+      const uintptr_t r = reinterpret_cast<uintptr_t>(s.rows), z = r + size_t(s.slices) * s.width * 8;
+      for (const NormSum& o : {a, b})
+        if (o.width) CHECK(r >= reinterpret_cast<uintptr_t>(o.part) + size_t(o.n) * o.width * 4);
+      if (a.slices > 1 && b.slices > 1)
+        CHECK(reinterpret_cast<uintptr_t>(b.rows) >= reinterpret_cast<uintptr_t>(a.rows) + size_t(a.slices) * a.width * 8);
+      CHECK(r % 8 == 0 && z <= end);
+      ++g_sliced;
+    }
     // every partial row summed is one that the launch before has written
     const uintptr_t p0 = reinterpret_cast<uintptr_t>(s.part);
     int64_t rows = 0;
@@ -308,6 +321,7 @@ int main() {
   forward_calls();
   gradient_calls();
   shares();
+  CHECK(g_sliced > 20);
   std::printf("norm driver: all checks passed\n");
   return 0;
 }
