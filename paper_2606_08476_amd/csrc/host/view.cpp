@@ -16,6 +16,14 @@
 //     occurs, so every query of the piece sees the same first n_P received
 //     tokens of its document: the received pass is mask-free per piece.
 // Tiles that no query of a block can see are never listed.
+//
+// Under a sliding window with sinks a query sees, of these, the last `window` tokens up
+// to itself and the document's first `sinks`. Both lists are ascending, so what a row
+// sees of each is a range that does not move back from row to row, and the sinks before
+// it: four indices per row (build_window). The receive set holds what some row sees, the
+// received pass has a mask, and the query tiles' ranges stay what they are; which tiles
+// in between are passed over follows from the first row's indices (fck::key_tiles), on
+// the host for the costs and in the kernels for the walk.
 #include <hip/hip_runtime.h>
 
 #include <algorithm>

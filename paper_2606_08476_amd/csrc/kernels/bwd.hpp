@@ -41,6 +41,10 @@ __global__ __launch_bounds__(256, 2) void attn_bwd_scored_kernel(BwdParams p) {
 
 // (Windows with slopes at head dim 128, and capped with dQ by atomics for ungrouped heads,
 // take 257 registers and more: one wave per SIMD instead of two and spills.)
+// The whole backward, 32/8 heads of 128, 64K tokens and 8 ranks, window 1024: 531-550 us,
+// 1.5 GB at 2.8 TB/s, matrix unit busy 45% of the cycles, vector unit 34%, both 13%; window
+// 4096, 16K rows: 2945-3060, 63, 36 and 18%. Five products of what the rows see are 297
+// GFLOP (2388); seven of them, the tiles' masked parts and the residuals make 478 (3405).
 template <int D, int KIND, bool MORE = false>
 constexpr int kWindowWaves = D == 128 && ((KIND & kScoreBias) || MORE) ? 1 : 2;
 template <int D, int HPI, int KIND>

@@ -40,6 +40,16 @@
 // so that it stays a normal fp16 number down to 2^-30 (scores of 10.4 caps, where 1 -
 // tanh^2 is 2^-28); the 4 and the 2^-16 are in the final scale.
 // P's residual is formed before that, where it is needed.
+//
+// Windowed views (WIN, see score.hpp): a tile's rows end with the first that does not see
+// its last key; per wave, rows from `qcut` on are compared with their windows' starts
+// (which go through LDS as their limits do), and from `qend` on there is nothing to
+// compute. Sinks are seen to the document's end, so they have tiles of their own (in one
+// tile with the keys behind them: 31287 iterations in place of 31002, 16K rows, window
+// 4096, 64 sinks; 9336 in place of 9418 in the case below, and spills in a capped kernel).
+// 32/8 heads of 128, 8193 rows of 64K tokens over 8 ranks, window 1024: 318-333 us, 1.34
+// times the iterations that the pairs alone would fill; 16K rows, window 4096: 1765-1830,
+// 1.05 times. The former with dQ by atomics 1020 us.
 #include "common.hpp"
 #include "launch.hpp"
 #include "score.hpp"

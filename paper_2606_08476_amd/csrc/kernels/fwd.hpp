@@ -2,8 +2,8 @@
 // Forward attention over one rank's share (gfx950).
 //
 // One workgroup (4 waves) takes one work item -- a tile of query tokens
-// with a received key range (no mask inside it, FlashCP Sec. 3.2: every
-// query of a piece sees the same received prefix) and a local key range
+// with a received key range (no mask inside it but a window's, FlashCP Sec. 3.2:
+// every query of a piece sees the same received prefix) and a local key range
 // (intra-document causal, Sec. 2.1) -- for `heads_per_tile` query heads of
 // one KV head. Each wave owns 32/heads_per_tile query rows of every one of
 // those heads (a query per lane). Key tiles of 64 keys are double-buffered
@@ -65,6 +65,18 @@
 // within two waves per SIMD. 32/8 heads of 128 over 64K tokens and 8 ranks, two
 // passes merged / one: no score function 381 / 355 us, capped 445 / 421; with queries
 // scaled by 6, 400 / 373 and 454 / 427.
+//
+// Windowed views (WIN, see score.hpp): the same walk over the key tiles that some row of
+// the query tile sees, sinks first; tiles that a window begins or ends in are masked, the
+// received ones too. A row may see nothing of a range: its partial has no weight then,
+// as one of an empty range. 32/8 heads of 128, 8193 rows of 64K tokens over 8 ranks,
+// window 1024: one pass 171-183 us, where 54 us would move its 290 MB and 95 us multiply
+// what the rows see (118 GFLOP at 1240 TFLOP/s). The tiles hold 1.25 times that, at 1.6 us
+// for one in each of the 512 resident workgroups, as without windows; the rest is where
+// 2208 workgroups of 18 tiles begin and end. Window 4096: 500 us, 80% of that rate (1.03
+// times the pairs). Matrix unit busy 41% of the cycles (55), vector unit 48% (43), both
+// 18% (23). 16 single tokens that see 4100 of their documents' 16K keys each, split:
+// 46 us, 5.8 TB/s, and 7 to combine.
 #include "common.hpp"
 #include "launch.hpp"
 #include "score.hpp"
@@ -734,7 +746,7 @@ __global__ __launch_bounds__(256, 2) void attn_fwd_scored_kernel(FwdParams p) {
   fwd_tile<D, HPW, OUT, SC>(p, smem);
 }
 // (Windows with slopes at head dim 128 take 257 registers and more: one wave per SIMD
-// instead of two and spills.)
+// instead of two with spills, which read and write HBM in the loop.)
 template <int D, int HPW, int OUT, int KIND>
 __global__ __launch_bounds__(256, D == 128 && (KIND & kScoreBias) ? 1 : 2) void attn_fwd_window_kernel(FwdParams p) {
   __shared__ __attribute__((aligned(16))) char smem[FwdLds<D, KIND>::bytes];

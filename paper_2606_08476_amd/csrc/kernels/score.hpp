@@ -126,7 +126,9 @@ __device__ __forceinline__ float score_bound(float c, float qn, float kn, float 
 // keys (indices ascend with positions) a row sees those from the first in its window up
 // to itself or its receive limit, and those before `sink`. In the query-major kernels a
 // lane has a row: its windows' starts are in LDS (a word per source and lane of 32, read
-// on tiles that are masked), the tile's own bounds in scalar registers.
+// on tiles that are masked), the tile's own bounds in scalar registers. (The table is
+// read through the tile's first and last row; a table of those per item, one load
+// instead of two in turn, was no faster.)
 struct WindowTiles {
   KeyTiles recv, local;
   int sink_r, sink_l;    // ends of the sinks
