@@ -10,6 +10,7 @@ fails with an error.
 from __future__ import annotations
 
 import ctypes as C
+import operator
 import os
 import struct
 
@@ -291,6 +292,9 @@ class View:
         s, sp, m = _shards(plan)
         h = P()
         t = C.byref(TileCfg(*[int(x) for x in tiles])) if tiles is not None else None
+        window, sinks = operator.index(window), operator.index(sinks)
+        if max(abs(window), abs(sinks)) > 0x7fffffff:
+            raise ValueError(f"window {window} or sinks {sinks} does not fit 32 bits")
         if cap or slopes is not None or window or sinks:
             f = None
             if slopes is not None:
@@ -300,7 +304,7 @@ class View:
                 f = f if f.flags.aligned else f.copy()
             score = Score(float(cap), None if f is None else f.ctypes.data)
             _check(_addr().fc_view_create_windowed(p, n, sp, m, cp, rank, hq, hkv, d, t, C.byref(score),
-                                                   C.byref(Window(int(window), int(sinks))), C.byref(h)))
+                                                   C.byref(Window(window, sinks)), C.byref(h)))
         else:
             _check(_addr().fc_view_create(p, n, sp, m, cp, rank, hq, hkv, d, t, C.byref(h)))
         self._h = h
