@@ -215,30 +215,27 @@ __device__ __forceinline__ void load_weights(float (&wa)[V], float (&wb)[V], con
   }
 }
 
-// Sine and cosine of a turn's 64-bit fraction, within 0.72 steps: the nearest quarter
-// turns off, |x| <= pi / 4 in two parts x + e, and
-//   sin = x + (e - x^3/6 + x^5/120 - ..),  cos = 1 - x^2/2 + (x^4/24 - .. - x e),
-// Taylor's series to x^9 and x^10 (what is left out is under 2^-28), the last sums of a large
-// and a small part. (With sincospif of the fraction as fp32 1.5 times as many of the bf16
-// results are not the nearest, 0.0042 % and not 0.0028 % of 16K rows; both take as long.)
+// Sine and cosine of a turn's 64-bit fraction, the nearest fp32 values but for one in two
+// thousand: the nearest quarter turns off, |x| <= pi / 4, Taylor's series to x^11 and x^12
+// in 64 bits (what is left out is under 2^-36). The calls take as long as with sincospif of
+// the fraction as fp32, or with sums in 32-bit pairs: a row's heads share its sines.
 __device__ __forceinline__ void turn_sincos(uint64_t turn, float& sn, float& cs) {
-#pragma clang fp contract(off)
-  const uint32_t top = uint32_t(turn >> 32), quarter = (top + 0x20000000u) >> 30;
-  const int32_t h = int32_t(top - (quarter << 30));  // 2^-32 turns, -2^29 .. 2^29
-  constexpr float k = 0x1.921fb6p-30f, kl = -0x1.777a5cp-55f;  // 2 pi 2^-32 in two parts
-  const float f = float(h), fl = float(h - int32_t(f));
-  const float x = f * k;
-  const float e = __builtin_fmaf(f, k, -x) + __builtin_fmaf(f, kl, fl * k);
-  const float z = x * x, zl = __builtin_fmaf(x, x, -z);
-  float p = __builtin_fmaf(z, 0x1.71de3ap-19f, -0x1.a01a02p-13f);  // 1/9!, -1/7!
-  p = __builtin_fmaf(z, p, 0x1.111112p-7f);                        // 1/5!
-  p = __builtin_fmaf(z, p, -0x1.555556p-3f);                       // -1/3!
-  const float s0 = x + __builtin_fmaf(x * z, p, __builtin_fmaf(-0.5f * z, e, e));
-  float q = __builtin_fmaf(z, -0x1.27e4fcp-22f, 0x1.a01a02p-16f);  // -1/10!, 1/8!
-  q = __builtin_fmaf(z, q, -0x1.6c16c2p-10f);                      // -1/6!
-  q = __builtin_fmaf(z, q, 0x1.555556p-5f);                        // 1/4!
-  const float t = 1.f - 0.5f * z, tl = (1.f - t) - 0.5f * z;
-  const float c0 = t + __builtin_fmaf(z * z, q, tl - __builtin_fmaf(x, e, 0.5f * zl));
+  const uint32_t quarter = uint32_t((turn + (uint64_t(1) << 61)) >> 62);
+  const uint64_t h = turn - (uint64_t(quarter) << 62);  // 2^-64 turns, -2^61 .. 2^61
+  constexpr double k = 6.283185307179586476925286766559 * 0x1p-32;
+  const double x = __builtin_fma(double(int32_t(h >> 32)), k, double(uint32_t(h)) * (k * 0x1p-32));
+  const double z = x * x;
+  double p = __builtin_fma(z, -1.0 / 39916800, 1.0 / 362880);
+  p = __builtin_fma(z, p, -1.0 / 5040);
+  p = __builtin_fma(z, p, 1.0 / 120);
+  p = __builtin_fma(z, p, -1.0 / 6);
+  const float s0 = float(__builtin_fma(x * z, p, x));
+  double q = __builtin_fma(z, 1.0 / 479001600, -1.0 / 3628800);
+  q = __builtin_fma(z, q, 1.0 / 40320);
+  q = __builtin_fma(z, q, -1.0 / 720);
+  q = __builtin_fma(z, q, 1.0 / 24);
+  q = __builtin_fma(z, q, -0.5);
+  const float c0 = float(__builtin_fma(z, q, 1.0));
   const bool swap = quarter & 1;
   const float a = swap ? c0 : s0, b = swap ? s0 : c0;
   sn = quarter & 2 ? -a : a;
