@@ -86,10 +86,11 @@ int32_t View::first_row_beyond(int32_t s, int src, int32_t k) const {
 // positions above p - window, up to its own, and those below `sinks`. Both lists are in
 // the order of their positions, so that a window is a range of each, which does not move
 // back from row to row. A document that ends within the window of its last row has no
-// sinks but what every row sees anyway.
+// sinks but what every row sees anyway; if all do, the view is one without a window, but
+// where scores are capped alone: the windowed kernels' P suit rows of few keys (fwd.hpp).
 void View::build_window(const int32_t* cu) {
   win.clear();
-  windowed = false;
+  windowed = window && cap > 0 && slopes.empty() && !q_gpos.empty();
   if (!window) return;
   win.resize(4 * q_gpos.size());
   pairs_loc = pairs_recv = 0;

@@ -97,3 +97,30 @@ def test_two_calls_at_once(dev):  # noqa: F811
                 got.append(step(x))
     torch.cuda.synchronize()
     assert all(W.same(want, g) for g in got)
+
+
+@pytest.mark.parametrize("window", [3, 500])
+@pytest.mark.parametrize("hq,hkv,d", [(8, 2, 128), (4, 4, 64)])
+def test_capped_rows_of_a_single_key(window, hq, hkv, d, dev):  # noqa: F811
+    """A row that sees one key has that key's value for O, whatever its P was rounded to,
+    and no gradient in its score: in windows that end in the documents and in ones that
+    reach over them. O's only rounding is then the product with 1 / P, in fp32: a step."""
+    shape = dict(lens=[1] * 40 + [5, 300, 1, 7], cp=1, rank=0, hq=hq, hkv=hkv, d=d, plan="whole_lpt")
+    r = W.Run(shape, (window, 0), "cap30", dev)
+    want, b = r.oracle(dout=r.do)
+    one = r.pos[0] == 0
+    for mode in (F.FC_TWO_PASS, F.FC_FUSED):
+        o, o32, lse = r.forward(mode)
+        near("o", o, want["o"], b["o"])
+        near("lse", lse, want["lse"], b["lse"])
+        v = r.kv[1][one].repeat_interleave(hq // hkv, 1).float()
+        assert bool(((o32[one] - v).abs() <= 2.0 ** -22 * v.abs()).all())
+    o, o32, lse = r.forward(F.FC_TWO_PASS)
+    g = r.grads()
+    F.fc_attn_bwd(r.view, r.q, *r.kv, o, lse, r.do, 0.0, *g, r.u8(r.view.workspace_size()[1]), o_f32=o32)
+    torch.cuda.synchronize()
+    W.check_grads("bwd", r, g, want, b)
+    # dS = P (dP - D): sums of d products of dO and O, which are the same within fp32
+    size = (r.do[one].float().abs() * v.abs()).sum(-1) * (d + 4) * 2.0 ** -23
+    k = r.kv[0][one].repeat_interleave(hq // hkv, 1).float().abs()
+    assert bool((g[0][one].abs() <= size[..., None] * k).all())
