@@ -280,7 +280,7 @@ int run(const View& v, const fc_rope* rope, std::initializer_list<Set> sets, boo
     p.pairs = rope->dim / 2;
     p.packed_pos = rope->packed_pos != 0;
     p.amplitude = rope->amplitude;
-    for (int32_t i = 0; i < p.pairs; ++i) p.turn[i] = turns(rope->inv_freq[i]);
+    turns(rope->inv_freq, p.pairs, p.turn);
     layout = rope->interleaved ? fck::kRopeNeighbours
              : p.pairs % 8     ? fck::kRopeHalvesOdd
                                : fck::kRopeHalves;

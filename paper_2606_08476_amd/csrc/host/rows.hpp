@@ -39,12 +39,15 @@ inline int check_rope(const fc_rope* r, int32_t d) {
 }
 
 // Radians per position as turns modulo 1, 64-bit fixed point (|w| is within
-// FC_ROPE_FREQ_MAX, checked before).
-inline uint64_t turns(double w) {
+// FC_ROPE_FREQ_MAX, checked before). (Long doubles are truncated without a change of the
+// rounding mode by SSE3's store alone: with such changes n = 32 take up to 1.2 us.)
+__attribute__((target("sse3"))) inline void turns(const double* w, int32_t n, uint64_t* turn) {
   constexpr long double kPerTurn = 0.15915494309189533576888376337251436L;
-  const long double t = w * kPerTurn;
-  const long double f = t - static_cast<int>(t);  // of w's sign, exact
-  return static_cast<uint64_t>(static_cast<int64_t>(f * 9223372036854775808.0L)) << 1;
+  for (int32_t i = 0; i < n; ++i) {
+    const long double t = w[i] * kPerTurn;
+    const long double f = t - static_cast<int>(t);  // of w's sign, exact
+    turn[i] = static_cast<uint64_t>(static_cast<int64_t>(f * 9223372036854775808.0L)) << 1;
+  }
 }
 
 }  // namespace fc
