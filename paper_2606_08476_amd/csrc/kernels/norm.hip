@@ -17,9 +17,9 @@
 // of its sums (a gather of 135K rows of 8x128 keys and values 215 -> 208 us), and the
 // weights without a wait for each (208 -> 192).
 // Measured, with cold inputs (a copy of 256 MiB: 5.4 TB/s): 8193 rows of 32/8x128
-// queries, keys and values, 201 MB, 34-43 us, 4.7-5.9 TB/s; that gather, 1107 MB, 198 us,
-// 5.6 TB/s; gradients of 8193 query rows and 53237 key rows (32/8x128), 1033 MB, 186 us,
-// 5.5 TB/s, and 10 us more for the weights' sums. The smallest calls are latency: 5.2 us
+// queries, keys and values, 201 MB, 34-43 us, 4.7-5.9 TB/s; that gather, 1107 MB, 192-204
+// us, 5.4-5.8 TB/s; gradients of 8193 query rows and 53237 key rows (32/8x128), 1033 MB,
+// 181-190 us, 5.4-5.7 TB/s, and 10 us more for the weights' sums. The smallest calls are latency: 5.2 us
 // for 1024 rows of 4/4x64, a launch's 3 us, then a read, the sums and a write in turn.
 // (More waves per SIMD by launch bounds, 8 forward or 7 backward, spill: 192 -> 295 us,
 // 190 -> 212 us.)
