@@ -239,7 +239,7 @@ typedef struct {
  * with slopes does not look for keys out of the bias's reach. What a row does not see has no
  * weight in it; inputs are finite, as for every view. Where every document ends
  * within the window of its last row here, the view is the one without a window (but
- * that O is rounded otherwise if scores are capped alone). */
+ * that the P of O are rounded otherwise, as accurately, if scores are capped alone). */
 int fc_view_create_windowed(const int32_t* cu_seqlens, int32_t n_docs, const fc_shard* shards,
                             int64_t n_shards, int32_t cp, int32_t rank, int32_t hq, int32_t hkv,
                             int32_t d, const fc_tile_cfg* tiles, const fc_score* score,

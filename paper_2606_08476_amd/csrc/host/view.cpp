@@ -87,7 +87,7 @@ int32_t View::first_row_beyond(int32_t s, int src, int32_t k) const {
 // the order of their positions, so that a window is a range of each, which does not move
 // back from row to row. A document that ends within the window of its last row has no
 // sinks but what every row sees anyway; if all do, the view is one without a window, but
-// where scores are capped alone: the windowed kernels' P suit rows of few keys (fwd.hpp).
+// where scores are capped alone: with a window these take row maxima, cut or not.
 void View::build_window(const int32_t* cu) {
   win.clear();
   windowed = window && cap > 0 && slopes.empty() && !q_gpos.empty();

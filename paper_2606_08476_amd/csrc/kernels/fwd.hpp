@@ -108,12 +108,9 @@ __device__ __forceinline__ void fwd_tile(const FwdParams& p, char* smem) {
   constexpr bool WIN = KIND & kWindow;
   constexpr bool LEAN = KIND != 0;  // registers are short: lane's values counted where needed
   constexpr bool CAP = SC & kScoreCap, BIAS = SC & kScoreBias;
-  // capped scores alone lie within the cap: the exponentials of every row have one
-  // reference (cap_top), and neither maxima nor rescaling are needed
-  // (not windowed: in a row of few keys, none of which has then a P of 1, every P's rounding
-  // counts. With a maximum a single key's value comes out whole, and so D, and a dS of 0:
-  // gradients of short windows and documents were up to 0.014 off in the norm, and are
-  // 0.003, as uncapped ones.)
+  // capped scores alone lie within the cap: the exponentials of a row keep the reference
+  // that its first tile gives (set_top), and neither maxima nor rescaling are needed
+  // (not windowed: a row may see nothing of the first tile)
   constexpr bool FIXED = SC == kScoreCap && !WIN;
   constexpr bool FINAL = OUT == kOutFinal, MERGED = OUT == kOutMerged, UNIT = OUT == kOutUnit;
   constexpr bool CHUNKS = OUT == kOutChunks;
@@ -270,12 +267,13 @@ __device__ __forceinline__ void fwd_tile(const FwdParams& p, char* smem) {
 #pragma unroll
   for (int db = 0; db < DB; ++db) oacc[db] = zero16();
   float m = -INFINITY;  // reference row maximum (scaled, log2 units)
+  float top = 0.f;      // FIXED: exponent of a score at the cap
   float lsum = 0.f;     // this lane's share of the row sum
 
   // LSE of a row with sum `tot`, natural log (BIAS: and what rounding left out of the
   // row's share, from values read again rather than held across the loop)
   auto row_lse = [&](float tot) {
-    float l = (FIXED ? cap2 - p.cap_top : m) + __log2f(tot);
+    float l = (FIXED ? cap2 - top : m) + __log2f(tot);
     if constexpr (BIAS) {
       const int ln = int(fresh_lane()) & 31, r = min(q0 + wave * RPW + ln % RPW, q1 - 1);
       float rest;
@@ -502,6 +500,23 @@ __device__ __forceinline__ void fwd_tile(const FwdParams& p, char* smem) {
       for (int i = 0; i < 16; ++i) mx = fmaxf(mx, s[mb][i]);
     return SC ? max_halves(mx) : max_halves(mx) * c;
   };
+  // FIXED: the reference of the rows' exponentials, from a source's (or chunk's) first tile,
+  // masked: cap_top, moved by at most a half so that the tile's best key has a whole
+  // exponent. Its P is then a power of two, which bf16 holds: a single key's value comes out
+  // whole, and so D, and a dS of 0. (With cap_top itself, documents of two or three tokens:
+  // O 0.0020 off in the norm, dQ 0.0047, dK 0.0044; so 0.0012, 0.0019 and 0.0009, as
+  // uncapped. 500 to 900 tokens: O 0.0023, so 0.0020.) What is left is fp32's rounding of
+  // `top` and of the exponent, 2^-19 each. A row that sees nothing of the tile: any
+  // reference does. It takes no time that shows: a forward of 32/8 heads of 128 over 64K
+  // tokens and 8 ranks 441-443 us with it and without.
+  auto set_top = [&](const f32x16 (&s)[2]) {
+    float r0 = 1.f;
+#pragma unroll
+    for (int e = 0; e < 32; ++e) r0 = fminf(r0, s[e / 16][e % 16]);
+    r0 = -max_halves(-r0);
+    const float n = __builtin_rintf(__builtin_fmaf(r0, -2.f * cap2, p.cap_top));
+    top = __builtin_fmaf(r0, 2.f * cap2, n);
+  };
 
   wait_async();
   __syncthreads();
@@ -518,7 +533,10 @@ __device__ __forceinline__ void fwd_tile(const FwdParams& p, char* smem) {
       }
     }
     mask(sa, 0);
-    if constexpr (!FIXED) mxa = row_max(sa);
+    if constexpr (FIXED)
+      set_top(sa);
+    else
+      mxa = row_max(sa);
   }
   // every wave has read K of tile 0 before iteration 0 copies tile 2 into
   // the same buffer
@@ -546,13 +564,17 @@ __device__ __forceinline__ void fwd_tile(const FwdParams& p, char* smem) {
     constexpr uint32_t KN = (1 - PAR) * TILE, VC = (2 + PAR) * TILE;
     if (j + 1 < n_t) fetch(j + 1, (3 - PAR) * TILE, true);   // V of tile j+1
     if (j + 2 < n_t) fetch(j + 2, PAR * TILE, false);        // K of tile j+2
-    if (PAIRED && j == n_r) switch_source();
+    if (PAIRED && j == n_r) {
+      switch_source();
+      if (FIXED && active) set_top(sc);
+    }
     if (CHUNKS && j == chunk_end) {
       const bool recv = j <= n_r;
       const int c0 = recv ? 0 : n_r;  // the source's first key tile
       if (active) finish_chunk(recv, WIN ? first_chunk : j - c0 <= p.chunk, j == n_r, false);
       first_chunk = j == n_r;
       chunk_end = next_chunk(j);
+      if (FIXED && active) set_top(sc);
     }
     if (active) {
       // a row's output is rescaled only when its maximum grows by more than
@@ -604,7 +626,7 @@ __device__ __forceinline__ void fwd_tile(const FwdParams& p, char* smem) {
 #pragma unroll
           for (int e = n * EX; e < (n + 1) * EX; ++e) {
             const float y = sc[e / 16][e % 16];
-            const float x = __builtin_amdgcn_exp2f(FIXED ? __builtin_fmaf(y, -2.f * cap2, p.cap_top)
+            const float x = __builtin_amdgcn_exp2f(FIXED ? __builtin_fmaf(y, -2.f * cap2, top)
                                                    : SC  ? y - mref
                                                          : __builtin_fmaf(y, c, -mref));
             sc[e / 16][e % 16] = x;
