@@ -235,11 +235,12 @@ typedef struct {
  * view's receive set is what its queries see: every call below that fills, reads or
  * writes received rows takes them so. Key tiles out of every row's window are visited by
  * no call; the partial passes see the window's part of their source (a row without any:
- * O = 0, LSE = -inf). fc_plan_stats and the planners know nothing of windows. A window
- * with slopes does not look for keys out of the bias's reach. What a row does not see has no
- * weight in it; inputs are finite, as for every view. Where every document ends
- * within the window of its last row here, the view is the one without a window (but
- * that the P of O are rounded otherwise, as accurately, if scores are capped alone). */
+ * O = 0, LSE = -inf). fc_plan_stats and the planners know nothing of windows. With slopes,
+ * keys out of reach are left out within windows too, where these promise it. What a row
+ * does not see has no weight in it; inputs are finite, as for every view. Where every
+ * document ends within the window of its last row here, the view is the one without a
+ * window (but that the P of O are rounded otherwise, as accurately, if scores are capped
+ * alone). */
 int fc_view_create_windowed(const int32_t* cu_seqlens, int32_t n_docs, const fc_shard* shards,
                             int64_t n_shards, int32_t cp, int32_t rank, int32_t hq, int32_t hkv,
                             int32_t d, const fc_tile_cfg* tiles, const fc_score* score,

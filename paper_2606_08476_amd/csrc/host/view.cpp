@@ -512,14 +512,22 @@ void View::build_fwd_split() {
 // Whether looking for keys out of reach pays: it reads every row once more, and
 // leaves out, of each KV head's keys, what lies beyond the reach of the least steep
 // head of the group. Estimated for products of unit normal rows (whose bound is
-// log2(e) sqrt(d)); worth it from a tenth of the pairs on. Then also in which order
-// the forward takes its heads: by which the last workgroup, started when all before
-// it have been dealt to the resident slots, ends sooner (heads one after the other
-// run 8% slower, see score.hpp).
+// log2(e) sqrt(d)); worth it from a tenth of the pairs on. Windowed views have fewer
+// pairs for each row that is read, and heads of unequal reach: worth it from three tenths of
+// the pairs and two tiles' keys per row on. (64K tokens over 8 ranks, 32/8 heads of 128,
+// forward in one pass + backward: slopes of 0.5, windows of 256, 22% and 97 keys, 166 + 491
+// us without, 180 + 488 with; of 512, 55% and 368, 211 + 649 and 176 + 522; slopes of 4,
+// windows of 128, 55% and 163, 136 + 388 and 128 + 335; slopes from 2^-1/4 to 2^-8,
+// windows of 1024, 19% and 195, 280 + 897 and 315 + 883; of 4096, 36% and 745, 479 + 1525
+// and 451 + 1242. 32K tokens over 4, 16/8 heads of 64, slopes of 0.5, windows of 256, 26%
+// and 112, 42 + 112 and 49 + 118; of 512, 57% and 377, 52 + 139 and 47 + 122.) Then also
+// in which order the forward takes its heads: by which the last workgroup, started when
+// all before it have been dealt to the resident slots, ends sooner (heads one after the
+// other run 8% slower, see score.hpp).
 void View::decide_prune() {
   prune = far_first = false;
   kept = 1;
-  if (!biased || windowed || hq > fck::kNormHeads) return;
+  if (!biased || hq > fck::kNormHeads) return;
   const double bound = 2 * 1.4427 * std::sqrt(double(d)) + 100;
   std::vector<double> far(static_cast<size_t>(hkv));
   for (int32_t g = 0; g < hkv; ++g) {
@@ -532,12 +540,16 @@ void View::decide_prune() {
   std::iota(order.begin(), order.end(), 0);
   auto keys = [&](int32_t i) {
     const int32_t* it = &fwd_fused[8 * size_t(i)];
+    if (windowed) return double(bn_fwd) * (keys_of(it, 1).n + keys_of(it, 0).n);
     return double(it[3] - it[2]) + (it[5] - it[4]);
   };
   std::stable_sort(order.begin(), order.end(), [&](int32_t a, int32_t b) { return keys(a) > keys(b); });
-  // (keys by distance, evenly over the document up to the tile)
+  // (keys by distance, evenly over the document up to the tile; windowed: over the
+  // window, in whole tiles)
   auto seen = [&](int32_t i, double r) {
-    return keys(i) * std::min(1.0, r / std::max(1.0, double(q_pos[size_t(fwd_fused[8 * size_t(i)])])));
+    const double at = double(q_pos[size_t(fwd_fused[8 * size_t(i)])]);
+    if (windowed) return keys(i) * std::min(1.0, (r + bn_fwd) / (std::min(at, double(window)) + bn_fwd));
+    return keys(i) * std::min(1.0, r / std::max(1.0, at));
   };
   double all = 0, some = 0, turn_end = 0, first_end = 0, dealt = 0;
   for (int32_t i : order)
@@ -549,7 +561,7 @@ void View::decide_prune() {
       turn_end = std::max(turn_end, dealt / kSlotsResident + x);
       dealt += x * head_chunks();
     }
-  prune = some < 0.9 * all;
+  prune = windowed ? some < 0.7 * all && all - some >= 2.0 * bn_fwd * hkv * t_q() : some < 0.9 * all;
   if (!prune) return;
   kept = some / all;
   dealt = 0;

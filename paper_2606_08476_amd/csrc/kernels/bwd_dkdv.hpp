@@ -116,7 +116,7 @@ __device__ __forceinline__ void dkdv_tile(const BwdParams& p, int b, char* smem)
   auto lane_here = [&]() { return LEAN ? fresh_lane() : opaque(uint32_t(lane)); };
   const int half = lane >> 5;
   int item;  // the launch list is in launch order
-  const int kvh = kv_head<BIAS && !WIN>(p, b, p.n_items, item);
+  const int kvh = kv_head<BIAS>(p, b, p.n_items, item);
   const int32_t* it = p.items + 8 * item;  // launch list
   const int k0 = it[0], k1 = it[1], q0 = it[2], qfull = it[4], src = it[5];
   int q1 = it[3];
@@ -138,7 +138,7 @@ __device__ __forceinline__ void dkdv_tile(const BwdParams& p, int b, char* smem)
   // BIAS: rows from this position on are out of reach of the tile's last key, for every
   // head of the group: none of the tile's keys has a weight in them
   float far = INFINITY;
-  if (BIAS && !WIN && p.norms) {
+  if (BIAS && p.norms) {
     float qn = 0.f, s2 = INFINITY;
     for (int i = 0; i < p.group; ++i) {
       qn = fmaxf(qn, head_norm(p.norms, kvh * p.group + i));
@@ -176,7 +176,7 @@ __device__ __forceinline__ void dkdv_tile(const BwdParams& p, int b, char* smem)
   // V rows of this lane's key as the B operand of dP = dO V^T
   bf16x8 vreg[KS];
 
-  if (BIAS && !WIN && p.norms)
+  if (BIAS && p.norms)
     q1 = __builtin_amdgcn_readfirstlane(first_at(p.q_pos, q0, q1, nextafterf(far, INFINITY)));
   const int ntile = (q1 - q0 + RPI - 1) / RPI;
   const int n_it = ntile * (p.group / HPI);

@@ -68,7 +68,7 @@ __device__ __forceinline__ void dq_tile(const DqParams& p, int b, char* smem) {
   const int lane = threadIdx.x & 63, wave = wave_id();
   const int half = lane >> 5;
   int rest;
-  const int kvh = kv_head<BIAS && !WIN>(p, b, p.n_items * p.head_chunks, rest);
+  const int kvh = kv_head<BIAS>(p, b, p.n_items * p.head_chunks, rest);
   const int hc = rest % p.head_chunks;
   const int32_t* it = p.items + 8 * (rest / p.head_chunks);
   const int q0 = it[0], q1 = it[1], r1 = it[3], l1 = it[5];
@@ -169,7 +169,7 @@ __device__ __forceinline__ void dq_tile(const DqParams& p, int b, char* smem) {
       oreg[ks] = lds_b128(smem, 2u * uint32_t(qb ^ (ks << 4)), 0);
     }
   }
-  if (BIAS && !WIN && p.norms) {
+  if (BIAS && p.norms) {
     // the ranges start, whole tiles on, at the first key within reach of a row of the
     // workgroup, given its LSE
     float n2 = 0.f;

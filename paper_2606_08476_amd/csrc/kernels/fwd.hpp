@@ -139,7 +139,7 @@ __device__ __forceinline__ void fwd_tile(const FwdParams& p, char* smem) {
   const int half = lane >> 5;
   const int b = blockIdx.x;
   int rest;
-  const int kvh = kv_head<BIAS && !WIN>(p, b, (UNIT ? p.n_units : p.n_items) * p.head_chunks, rest);
+  const int kvh = kv_head<BIAS>(p, b, (UNIT ? p.n_units : p.n_items) * p.head_chunks, rest);
   const int hc = rest % p.head_chunks;
   const int32_t* it = (UNIT ? p.units : p.items) + 8 * (rest / p.head_chunks);
   const int q0 = it[0], q1 = it[1], r1 = it[3], l1 = it[5];
@@ -176,7 +176,7 @@ __device__ __forceinline__ void fwd_tile(const FwdParams& p, char* smem) {
   };
   // BIAS, final output: the ranges start, whole tiles on, at the first key within
   // reach of a row of the workgroup (the rows' norms from their registers)
-  const bool cut = BIAS && !WIN && (FINAL || MERGED || (UNIT && p.o_bf16)) && p.norms;
+  const bool cut = BIAS && (FINAL || MERGED || (UNIT && p.o_bf16)) && p.norms;
   if (cut) {
     read_q();
     float n2 = 0.f;
