@@ -540,7 +540,10 @@ int fc_lse_merge(const float* o_a, const float* lse_a, const float* o_b, const f
  * fixed inputs (a query-major pass recomputes S and dP for dQ).
  * deterministic == 0: the key-major pass also adds dQ with fp32 atomics (no
  * recompute); dK/dV are still reproducible, dQ's last bits vary from run to
- * run with the order of the additions. */
+ * run with the order of the additions. On a windowed view its dQ is also less exact
+ * where rows see few keys: dS is rounded to bf16, as on other views, whereas the
+ * query-major pass adds the residuals of rows with a P above 1/16 there (windows of 3: dQ
+ * off by 0.0019 in the norm and 0.0008); and the mode is the slower one there. */
 int fc_attn_bwd(fc_view view, const void* q, const void* k_loc, const void* v_loc,
                 const void* k_recv, const void* v_recv, const void* o, const float* o_f32,
                 const float* lse, const void* dout, float scale, int32_t deterministic,
