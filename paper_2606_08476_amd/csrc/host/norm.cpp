@@ -50,9 +50,10 @@ int64_t width_of(const View& v, const fc_norm& n, int32_t heads) {
 
 // How workgroups share a tensor's rows: kNormSteps steps each, fewer where the whole call
 // would leave most of the card without work. (A backward's workgroup leaves a row of
-// partial weight gradients. Of 16, 8 and 4 steps: gradients of 64K tokens over 8 ranks,
-// 32/8 heads of 128, 208, 203 and 205 us; of 50K over 4, 16/8 heads of 64, weights per
-// head, fp32, 109, 101 and 98.)
+// partial weight gradients. Of 16, 8, 4 and 2 steps, with the weights' sums: gradients of
+// 64K tokens over 8 ranks, 32/8 heads of 128, 208, 196, 192 and 202 us; of 50K over 4, 16/8
+// heads of 64, weights per head, fp32, 108, 102, 98 and 104; own rows of the former 44, 43,
+// 41 and 43; a gather of 135K rows of 8x128 217, 205, 193 and 204.)
 int64_t share(fck::NormRows& k, int32_t d, bool back, int32_t steps) {
   const int32_t slots = 256 / fck::norm_lanes(d, back);
   k.head_groups = (k.heads + slots - 1) / slots;
