@@ -225,7 +225,7 @@ int fc_view_create_scored(const int32_t* cu_seqlens, int32_t n_docs, const fc_sh
                           int32_t d, const fc_tile_cfg* tiles, const fc_score* score, fc_view* out);
 
 /* Windows: a query sees the last `window` tokens of its document up to itself, and the
- * document's first `sinks` tokens (up to itself). */
+ * document's first `sinks` tokens (up to itself). Sinks are tokens, keys as any other. */
 typedef struct {
   int32_t window; /* 0: every earlier token */
   int32_t sinks;  /* 0 or more; 0 without a window */
@@ -433,7 +433,7 @@ int fc_rope_bwd(fc_view view, const fc_rope* rope, int32_t out_bf16, const fc_ro
 
 /* ----------------------------------------------------------------- head norms
  * The norm of a query's or key's head, x of d values: n = (x - m) / sqrt(mean (x -
- * m)^2 + eps), m = 0 or (centred) mean x, times (weight + offset). Then its rotation,
+ * m)^2 + eps), m = 0 or (centred) mean x, times (weight + offset); nothing is added. Then its rotation,
  * in the same pass, rounded once. Rows and gradients as for the rotary rows above;
  * statistics and products are fp32. */
 typedef struct {

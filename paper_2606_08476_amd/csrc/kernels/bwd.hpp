@@ -40,7 +40,9 @@ __global__ __launch_bounds__(256, 2) void attn_bwd_scored_kernel(BwdParams p) {
 }
 
 // (Windows with slopes at head dim 128, and capped with dQ by atomics for ungrouped heads,
-// take 257 registers and more: one wave per SIMD instead of two and spills.)
+// take over 256 registers: one wave per SIMD, without scratch memory. With slopes, two
+// waves with 6 to 24 registers spilled are faster: the case below, window 1024, 907 us and
+// 664, where windows alone take 550; window 4096, 1533 and 1115.)
 // The whole backward, 32/8 heads of 128, 64K tokens and 8 ranks, window 1024: 531-550 us,
 // 1.5 GB at 2.8 TB/s, matrix unit busy 45% of the cycles, vector unit 34%, both 13%; window
 // 4096, 16K rows: 2945-3060, 63, 36 and 18%. Five products of what the rows see are 297

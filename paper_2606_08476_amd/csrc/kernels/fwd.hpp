@@ -73,7 +73,7 @@
 // window 1024: one pass 171-183 us, where 54 us would move its 290 MB and 95 us multiply
 // what the rows see (118 GFLOP at 1240 TFLOP/s). The tiles hold 1.25 times that, at 1.6 us
 // for one in each of the 512 resident workgroups, as without windows; the rest is where
-// 2208 workgroups of 18 tiles begin and end. Window 4096: 500 us, 80% of that rate (1.03
+// 2208 workgroups of 15.9 tiles (18 at most) begin and end. Window 4096: 500 us, 80% of that rate (1.03
 // times the pairs). Matrix unit busy 41% of the cycles (55), vector unit 48% (43), both
 // 18% (23). 16 single tokens that see 4100 of their documents' 16K keys each, split:
 // 46 us, 5.8 TB/s, and 7 to combine.
@@ -771,8 +771,10 @@ __global__ __launch_bounds__(256, 2) void attn_fwd_scored_kernel(FwdParams p) {
   __shared__ __attribute__((aligned(16))) char smem[FwdLds<D, SC>::bytes];
   fwd_tile<D, HPW, OUT, SC>(p, smem);
 }
-// (Windows with slopes at head dim 128 take 257 registers and more: one wave per SIMD
-// instead of two with spills, which read and write HBM in the loop.)
+// (Windows with slopes at head dim 128 take over 256 registers: one wave per SIMD, without
+// scratch memory. Two waves with 1 to 28 registers spilled are faster: 32/8 heads of 128,
+// 64K tokens over 8 ranks, window 1024, one pass 293-305 us and 213, two passes 336 and
+// 234, where windows alone take 181 and 217; window 4096, 506 and 358, 537 and 368.)
 template <int D, int HPW, int OUT, int KIND>
 __global__ __launch_bounds__(256, D == 128 && (KIND & kScoreBias) ? 1 : 2) void attn_fwd_window_kernel(FwdParams p) {
   __shared__ __attribute__((aligned(16))) char smem[FwdLds<D, KIND>::bytes];
